@@ -46,6 +46,7 @@ extern "C" {
 #define OZFP4_EHIP        -6  /* a HIP runtime call failed                         */
 #define OZFP4_ESCRATCH    -7  /* ozfp4_dgemm_noalloc: device not set up, or the
                                  call needs more than OZFP4_SCRATCH_BYTES       */
+#define OZFP4_EWORKSPACE  -8  /* the caller's workspace is too small             */
 
 #define OZFP4_MIN_MODULI   2
 #define OZFP4_MAX_MODULI  27
@@ -199,6 +200,120 @@ int ozfp4_product(int op, int64_t m, int64_t n, int64_t k,
                   const void* A, int64_t a_rs, int64_t a_cs,
                   const void* B, int64_t b_rs, int64_t b_cs,
                   void* C, int64_t ldc, int count);
+
+/* ---- 8-bit floating-point products with a scale for each block of 128 --- */
+
+/* Largest inner dimension of the 8-bit products (keeps a block's operand
+ * offsets within 32 bits), and the largest number of 64 x 64 output tiles, or
+ * of 128 x 128 tiles to quantise, of a call (one launch). */
+#define OZFP4_MAX_K_F8   4194304
+#define OZFP4_MAX_TILES_F8 16777215
+/* Types of high-precision inputs and of outputs. */
+#define OZFP4_F32  0
+#define OZFP4_BF16 1
+#define OZFP4_F16  2
+/* 8-bit formats: e4m3 (largest value 448, NaN, no infinity), e5m2 (57344). */
+#define OZFP4_E4M3 0
+#define OZFP4_E5M2 1
+/* Scale types: FP32, or a power of two 2^(byte - 127) in one byte (E8M0). */
+#define OZFP4_SCALE_F32  0
+#define OZFP4_SCALE_E8M0 1
+
+/*
+ * A quantised matrix: element (i, j) stands for
+ *     value(i, j) * scale(i', j'),
+ * value (i, j) at values[i * rs + j * cs] (bytes; one stride is 1 and the
+ * other at least the extent that runs along it), scale (i', j') at
+ * scales[i' * srs + j' * scs] (in elements of the scale type, any strides
+ * >= 0). Along the axis that a product sums over, a scale covers 128
+ * elements (i' = i / 128 or j' = j / 128 there). Along the other it covers
+ * one (tile = 0, a scale per line of 128) or 128 as well (tile = 1).
+ */
+typedef struct {
+  void* values;
+  int64_t rs, cs;
+  void* scales;
+  int64_t srs, scs;
+  int32_t format;
+  int32_t tile;
+} ozfp4_f8_matrix;
+
+/*
+ * ozfp4_quantize_f8 -- X (rows x cols, OZFP4_F32/BF16/F16, element (i, j) at
+ * X[i * x_rs + j * x_cs], one stride 1) to 8-bit values and scales. For each
+ * block, with a the largest finite |x| in it and t the format's largest value:
+ *     FP32 scale:  S = 1 if a = 0, else max(fl32(a / t), 2^-126);
+ *     E8M0 scale:  S = 1 if a = 0, else the least 2^E >= a / t, E >= -126;
+ *     value        the format's nearest to the exact quotient x / S, ties to
+ *                  even. NaN stays NaN; an infinity is NaN in e4m3 and
+ *                  itself in e5m2.
+ * A block is 1 x 128 or, with the outputs' `tile`, 128 x 128; the last ones
+ * of a line may be shorter. along_cols (or null) gets blocks along the columns
+ * axis: values with cs = 1, rs >= cols. along_rows (or null) gets blocks along
+ * the rows axis: values with rs = 1, cs >= rows. So values are adjacent along
+ * the axis that a product will sum over; that stride is a multiple of 16 and
+ * the values are 16-byte aligned (else OZFP4_EINVAL), and bytes up to the
+ * multiple of 16 behind a line's end are overwritten. Both outputs have one format
+ * and one `tile`; both are made from one read of X. Asynchronous on the set
+ * stream, allocates nothing, and so can be captured into a graph.
+ */
+int ozfp4_quantize_f8(int64_t rows, int64_t cols, const void* X, int x_type, int64_t x_rs, int64_t x_cs,
+                      int scale_type, const ozfp4_f8_matrix* along_cols, const ozfp4_f8_matrix* along_rows);
+
+/*
+ * ozfp4_gemm_f8 -- C = A B for quantised A (m x k, scales along its columns)
+ * and B (k x n, scales along its rows):
+ *     C_ij = sum_b sA(i, b) sB(b, j) sum_{k in b} A_ik B_kj
+ * over blocks b of 128, summed in FP32 and rounded once to the type of C
+ * (element (i, j) at C[i * c_rs + j * c_cs], one stride 1, no overlap with A
+ * and B). accumulate: C (FP32) += A B. NaN and infinities propagate as in
+ * FP32 arithmetic. k = 0 writes zeros (adds nothing).
+ * Operands whose k values are adjacent, with lines 16-byte aligned and at
+ * most 2^23 bytes apart, are read in place; others are copied into the
+ * workspace first. workspace: device memory of at least the bytes that
+ * ozfp4_gemm_f8_workspace gives for the same arguments, 256-byte aligned,
+ * used by this call only (OZFP4_EWORKSPACE if too small); it may be null
+ * if that is 0. Asynchronous on the set stream, allocates nothing, and so can
+ * be captured into a graph.
+ * OZFP4_EKBOUND for k > OZFP4_MAX_K_F8.
+ */
+int ozfp4_gemm_f8(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A, const ozfp4_f8_matrix* B,
+                  int scale_type, void* C, int c_type, int64_t c_rs, int64_t c_cs, int accumulate,
+                  void* workspace, int64_t workspace_bytes);
+int ozfp4_gemm_f8_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A,
+                            const ozfp4_f8_matrix* B, int64_t c_rs, int64_t c_cs, int64_t* bytes);
+
+/*
+ * ozfp4_linear_f8 -- Y = Xq W^T: X (m x k) quantised as by ozfp4_quantize_f8
+ * along its columns (a scale per line, values of x_format), times the
+ * transpose of the quantised weights W (n x k, scales along its columns).
+ * Y as C above. Workspace and the rest as for ozfp4_gemm_f8.
+ */
+int ozfp4_linear_f8(int64_t m, int64_t n, int64_t k, const void* X, int x_type, int64_t x_rs, int64_t x_cs,
+                    int x_format, const ozfp4_f8_matrix* W, int scale_type, void* Y, int y_type, int64_t y_rs,
+                    int64_t y_cs, void* workspace, int64_t workspace_bytes);
+int ozfp4_linear_f8_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* W, int64_t y_rs,
+                              int64_t y_cs, int64_t* bytes);
+
+/*
+ * ozfp4_linear_f8_backward -- the gradients of that layer for the output
+ * gradient dY (m x n):
+ *     dX (m x k)  = dYq1 W,       dYq1 = dY quantised along its columns,
+ *     dW (n x k)  = dYq0^T Xq0,   dYq0, Xq0 = dY, X quantised along their rows,
+ * a scale per line of 128, values of dy_format for dY and of x_format for X. W
+ * has tile = 1 (its scales serve both directions). dX of dx_type, dW FP32;
+ * accumulate: dW is added to. Each output as C above; either may be null (not
+ * wanted). X and dY are of one type. Workspace and the rest as for
+ * ozfp4_gemm_f8.
+ */
+int ozfp4_linear_f8_backward(int64_t m, int64_t n, int64_t k, const void* dY, int64_t dy_rs, int64_t dy_cs,
+                             int dy_format, const void* X, int64_t x_rs, int64_t x_cs, int x_format,
+                             int x_type, const ozfp4_f8_matrix* W, int scale_type, void* dX, int dx_type,
+                             int64_t dx_rs, int64_t dx_cs, float* dW, int64_t dw_rs, int64_t dw_cs,
+                             int accumulate, void* workspace, int64_t workspace_bytes);
+int ozfp4_linear_f8_backward_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* W,
+                                       int64_t dx_rs, int64_t dx_cs, int64_t dw_rs, int64_t dw_cs,
+                                       int64_t* bytes);
 
 /* Stream for subsequent calls (a hipStream_t; NULL = the null stream). */
 int ozfp4_set_stream(void* stream);

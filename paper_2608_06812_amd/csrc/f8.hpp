@@ -1,0 +1,91 @@
+// 8-bit floating-point products with a scale for each block of 128: host
+// interface of the kernels in f8_quantize.hip, f8_pack.hip and f8_gemm.hip,
+// and the device helpers that they share.
+//
+// A quantised matrix holds e4m3 or e5m2 values and one scale for every block
+// of 128 along the contraction: per line (1 x 128) or per 128 x 128 tile.
+// "Line" is a row of the left operand and a column of the right one, so both
+// operands of a product are sets of lines of k values.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ozfp4 {
+
+constexpr int kF8Block = 128;             // contraction values of one scale
+constexpr int64_t kF8MaxLd = 1 << 23;     // bytes from line to line: a block's offsets fit 32 bits
+
+// The stream of ozfp4_set_stream.
+hipStream_t library_stream();
+
+// Lines of a quantised operand, a line's k values adjacent; scale of line i,
+// block b at s[(i >> shift) * sl + b * sk] (shift 7: one per 128 lines).
+struct F8Lines {
+  const uint8_t* x;
+  int64_t ld;
+  const void* s;
+  int64_t sl, sk;
+  int64_t lines;
+  int shift;
+  int fmt;
+};
+
+// C[p + q * ldc] (+)= sum over k; P's lines are the adjacent ones of C.
+struct F8Gemm {
+  F8Lines P, Q;
+  int64_t k;
+  void* C;
+  int64_t ldc;
+  int type;          // OZFP4_F32, OZFP4_BF16, OZFP4_F16
+  int accumulate;    // C is FP32 and added to
+  int pow2;          // scales are E8M0 bytes
+  int vec;           // four adjacent elements of C are aligned for one store
+  int stages;        // blocks of 128 a k range holds
+  int64_t part;      // elements from one range's C to the next (0: one range)
+};
+
+hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g);
+
+// Sum of `ranges` partial products (q * ldp + p, part elements apart) into C.
+struct F8Sum {
+  const float* x;
+  int64_t ldp, part, lines_p, lines_q;
+  int ranges;
+  void* C;
+  int64_t ldc;
+  int type, accumulate;
+};
+hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s);
+
+// Bytes (line, kk) at x[line * ls + kk * ks], one stride 1, to lines of k
+// adjacent bytes with line stride ld (a multiple of 16).
+struct F8Pack {
+  const uint8_t* x;
+  int64_t ls, ks, lines, k;
+  uint8_t* out;
+  int64_t ld;
+};
+hipError_t launch_f8_pack(hipStream_t st, const F8Pack* p, int count);   // count 1 or 2
+
+// X (rows x cols, columns adjacent, row stride ldx): along_cols writes values
+// q1[i * ld1 + j] with a scale per row and 128 columns at s1[i * s1l + b *
+// s1k], along_rows q0[j * ld0 + i] with a scale per column and 128 rows at
+// s0[j * s0l + b * s0k]; with `tile` one scale per 128 x 128, i and j there
+// counting tiles. A null q is not wanted.
+struct F8Quantize {
+  const void* x;
+  int64_t rows, cols, ldx;
+  int src, fmt, pow2, tile;
+  uint8_t* q1;
+  int64_t ld1;
+  void* s1;
+  int64_t s1l, s1k;
+  uint8_t* q0;
+  int64_t ld0;
+  void* s0;
+  int64_t s0l, s0k;
+};
+hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize& q);
+
+}  // namespace ozfp4

@@ -1,0 +1,376 @@
+// C entry points of the 8-bit floating-point products (contracts in
+// include/ozfp4.h): argument checks, workspace layout, launches. A workspace
+// query runs the same code as the call, without launching.
+#include <algorithm>
+
+#include "f8.hpp"
+#include "ozfp4.h"
+
+using namespace ozfp4;
+
+namespace {
+
+int64_t round_up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+int64_t blocks_of(int64_t v) { return (v + kF8Block - 1) / kF8Block; }
+
+// The caller's workspace, handed out in 256-byte steps; without launching
+// (`dry`) only the bytes are counted.
+struct Work {
+  uint8_t* base;
+  int64_t bytes, used;
+  bool dry;
+  uint8_t* take(int64_t n) {
+    uint8_t* p = base + used;
+    used += round_up(n, 256);
+    return p;
+  }
+  bool fits() const { return dry || used <= bytes; }
+};
+
+#define F8_LAUNCH(expr)                            \
+  do {                                             \
+    if ((expr) != hipSuccess) return OZFP4_EHIP;   \
+  } while (0)
+
+bool layout_ok(int64_t rows, int64_t cols, int64_t rs, int64_t cs) {
+  return (rs == 1 && cs >= std::max<int64_t>(1, rows)) || (cs == 1 && rs >= std::max<int64_t>(1, cols));
+}
+
+bool dims_ok(int64_t m, int64_t n, int64_t k) {
+  if (m < 0 || n < 0 || k < 0) return false;
+  auto ok = [](int64_t a, int64_t b) { return a == 0 || b <= OZFP4_MAX_ELEMENTS / a; };
+  return ok(m, n) && ok(m, k) && ok(n, k);
+}
+
+bool tiles_ok(int64_t rows, int64_t cols, int64_t tile) {
+  const int64_t a = (rows + tile - 1) / tile, b = (cols + tile - 1) / tile;
+  return a == 0 || b <= OZFP4_MAX_TILES_F8 / a;
+}
+
+bool type_ok(int t) { return t >= OZFP4_F32 && t <= OZFP4_F16; }
+bool format_ok(int f) { return f == OZFP4_E4M3 || f == OZFP4_E5M2; }
+bool scale_ok(int s) { return s == OZFP4_SCALE_F32 || s == OZFP4_SCALE_E8M0; }
+
+// A product's operand of the caller (rows x cols).
+int check_matrix(const ozfp4_f8_matrix* M, int64_t rows, int64_t cols) {
+  if (!M || !format_ok(M->format) || (M->tile != 0 && M->tile != 1)) return OZFP4_EINVAL;
+  if (!layout_ok(rows, cols, M->rs, M->cs) || M->srs < 0 || M->scs < 0) return OZFP4_EINVAL;
+  if (rows > 0 && cols > 0 && (!M->values || !M->scales)) return OZFP4_EINVAL;
+  return OZFP4_OK;
+}
+
+// Lines with any storage order: element kk of line i at l.x[i * l.ld + kk * ks].
+struct Operand {
+  F8Lines l;
+  int64_t ks;
+};
+
+// The rows of M (line = row, k along its columns), or its columns.
+Operand rows_of(const ozfp4_f8_matrix& M, int64_t rows) {
+  return {{static_cast<const uint8_t*>(M.values), M.rs, M.scales, M.srs, M.scs, rows, M.tile ? 7 : 0, M.format},
+          M.cs};
+}
+Operand cols_of(const ozfp4_f8_matrix& M, int64_t cols) {
+  return {{static_cast<const uint8_t*>(M.values), M.cs, M.scales, M.scs, M.srs, cols, M.tile ? 7 : 0, M.format},
+          M.rs};
+}
+
+bool in_place(const Operand& o, int64_t k) {
+  if ((o.ks != 1 && k > 1) || reinterpret_cast<uintptr_t>(o.l.x) % 16) return false;
+  return o.l.lines == 1 || (o.l.ld % 16 == 0 && o.l.ld <= kF8MaxLd);
+}
+
+// An output matrix of the caller.
+struct Out {
+  void* C;
+  int type;
+  int64_t rs, cs;
+  int accumulate;
+};
+
+int check_out(const Out& c, int64_t rows, int64_t cols) {
+  if (!type_ok(c.type) || !layout_ok(rows, cols, c.rs, c.cs)) return OZFP4_EINVAL;
+  if (c.accumulate && c.type != OZFP4_F32) return OZFP4_EINVAL;
+  return OZFP4_OK;
+}
+
+// C = A B from the rows of A and the columns of B.
+int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, const Out& c) {
+  if (A.l.lines == 0 || B.l.lines == 0 || (k == 0 && c.accumulate)) return OZFP4_OK;
+  F8Pack pack[2];
+  int packs = 0;
+  for (Operand* o : {&A, &B}) {
+    if (k == 0 || in_place(*o, k)) continue;
+    const int64_t ld = round_up(k, 128);
+    pack[packs++] = {o->l.x, o->l.ld, o->ks, o->l.lines, k, w.take(o->l.lines * ld), ld};
+    o->l.x = pack[packs - 1].out;
+    o->l.ld = ld;
+  }
+  F8Gemm g = {};
+  // the lines of the operand along which C is adjacent are the kernel's P
+  const bool row_major = c.cs == 1;
+  g.P = row_major ? B.l : A.l;
+  g.Q = row_major ? A.l : B.l;
+  g.k = k;
+  g.C = c.C;
+  g.ldc = row_major ? c.rs : c.cs;
+  g.type = c.type;
+  g.accumulate = c.accumulate;
+  g.pow2 = pow2;
+  const int64_t size = c.type == OZFP4_F32 ? 4 : 2;
+  g.vec = reinterpret_cast<uintptr_t>(c.C) % (4 * size) == 0 && g.ldc % 4 == 0;
+  g.stages = (int)std::max<int64_t>(1, blocks_of(k));
+  if (!w.fits()) return OZFP4_EWORKSPACE;
+  if (w.dry) return OZFP4_OK;
+  if (packs) F8_LAUNCH(launch_f8_pack(st, pack, packs));
+  F8_LAUNCH(launch_f8_gemm(st, g));
+  return OZFP4_OK;
+}
+
+// X as a caller gives it, and its quantisation into the workspace.
+struct Source {
+  const void* x;
+  int type;
+  int64_t rows, cols, rs, cs;
+};
+
+// A quantised set of lines in the workspace: scales with the lines adjacent.
+Operand take_lines(Work& w, int64_t lines, int64_t k, int fmt, int pow2) {
+  const int64_t ld = round_up(k, 128), nb = blocks_of(k);
+  Operand o = {};
+  o.l.ld = ld;
+  o.l.x = w.take(lines * ld);
+  o.l.s = w.take(lines * nb * (pow2 ? 1 : 4));
+  o.l.sl = 1;
+  o.l.sk = lines;
+  o.l.lines = lines;
+  o.l.fmt = fmt;
+  o.ks = 1;
+  return o;
+}
+
+int quantize(hipStream_t st, const Source& X, int fmt, int pow2, int tile, const Operand* along_cols,
+             const Operand* along_rows) {
+  F8Quantize q = {};
+  q.x = X.x;
+  q.src = X.type;
+  q.fmt = fmt;
+  q.pow2 = pow2;
+  q.tile = tile;
+  // a column-major X is read as its row-major transpose
+  const bool turned = X.cs != 1;
+  q.rows = turned ? X.cols : X.rows;
+  q.cols = turned ? X.rows : X.cols;
+  q.ldx = turned ? X.cs : X.rs;
+  const Operand* o1 = turned ? along_rows : along_cols;
+  const Operand* o0 = turned ? along_cols : along_rows;
+  if (o1) {
+    q.q1 = const_cast<uint8_t*>(o1->l.x);
+    q.ld1 = o1->l.ld;
+    q.s1 = const_cast<void*>(o1->l.s);
+    q.s1l = o1->l.sl;
+    q.s1k = o1->l.sk;
+  }
+  if (o0) {
+    q.q0 = const_cast<uint8_t*>(o0->l.x);
+    q.ld0 = o0->l.ld;
+    q.s0 = const_cast<void*>(o0->l.s);
+    q.s0l = o0->l.sl;
+    q.s0k = o0->l.sk;
+  }
+  F8_LAUNCH(launch_f8_quantize(st, q));
+  return OZFP4_OK;
+}
+
+int gemm(Work& w, int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A, const ozfp4_f8_matrix* B,
+         int pow2, const Out& c) {
+  if (!dims_ok(m, n, k) || !tiles_ok(m, n, 64)) return OZFP4_EINVAL;
+  if (k > OZFP4_MAX_K_F8) return OZFP4_EKBOUND;
+  int rc = check_matrix(A, m, k);
+  if (!rc) rc = check_matrix(B, k, n);
+  if (!rc) rc = check_out(c, m, n);
+  if (rc) return rc;
+  if (!w.dry && m > 0 && n > 0 && !c.C) return OZFP4_EINVAL;
+  return product(w, library_stream(), k, rows_of(*A, m), cols_of(*B, n), pow2, c);
+}
+
+int linear(Work& w, int64_t m, int64_t n, int64_t k, const Source& X, int fmt, const ozfp4_f8_matrix* W,
+           int pow2, const Out& y) {
+  if (!dims_ok(m, n, k) || !tiles_ok(m, n, 64) || !tiles_ok(m, k, 128)) return OZFP4_EINVAL;
+  if (k > OZFP4_MAX_K_F8) return OZFP4_EKBOUND;
+  int rc = check_matrix(W, n, k);
+  if (!rc) rc = check_out(y, m, n);
+  if (rc) return rc;
+  if (!w.dry) {
+    if (!type_ok(X.type) || !format_ok(fmt) || !layout_ok(m, k, X.rs, X.cs)) return OZFP4_EINVAL;
+    if (m > 0 && ((k > 0 && !X.x) || (n > 0 && !y.C))) return OZFP4_EINVAL;
+  }
+  if (m == 0 || n == 0) return OZFP4_OK;
+  const Operand x = take_lines(w, m, k, fmt, pow2);
+  if (!w.dry) {
+    Work rest = w;   // nothing is launched in a workspace that is too small
+    rest.dry = true;
+    rc = product(rest, nullptr, k, x, rows_of(*W, n), pow2, y);
+    if (rc) return rc;
+    if (rest.used > w.bytes) return OZFP4_EWORKSPACE;
+    rc = quantize(library_stream(), X, fmt, pow2, 0, &x, nullptr);
+    if (rc) return rc;
+  }
+  return product(w, library_stream(), k, x, rows_of(*W, n), pow2, y);
+}
+
+int backward(Work& w, int64_t m, int64_t n, int64_t k, const Source& dY, int dy_fmt, const Source& X, int x_fmt,
+             const ozfp4_f8_matrix* W, int pow2, bool want_dx, const Out& dx, bool want_dw, const Out& dw) {
+  if (!dims_ok(m, n, k) || !tiles_ok(m, k, 64) || !tiles_ok(n, k, 64) || !tiles_ok(m, n, 128))
+    return OZFP4_EINVAL;
+  if (m > OZFP4_MAX_K_F8 || n > OZFP4_MAX_K_F8) return OZFP4_EKBOUND;
+  int rc = check_matrix(W, n, k);
+  if (!rc && !W->tile) rc = OZFP4_EINVAL;
+  if (!rc && want_dx) rc = check_out(dx, m, k);
+  if (!rc && want_dw) rc = check_out(dw, n, k);
+  if (rc) return rc;
+  if (!w.dry) {
+    if (!type_ok(X.type) || !format_ok(dy_fmt) || !format_ok(x_fmt)) return OZFP4_EINVAL;
+    if (!layout_ok(m, n, dY.rs, dY.cs) || !layout_ok(m, k, X.rs, X.cs)) return OZFP4_EINVAL;
+    if (m > 0 && ((n > 0 && !dY.x) || (want_dw && k > 0 && !X.x))) return OZFP4_EINVAL;
+  }
+  Operand dy1 = {}, dy0 = {}, x0 = {};
+  if (want_dx) dy1 = take_lines(w, m, n, dy_fmt, pow2);
+  if (want_dw) {
+    dy0 = take_lines(w, n, m, dy_fmt, pow2);
+    x0 = take_lines(w, k, m, x_fmt, pow2);
+  }
+  hipStream_t st = library_stream();
+  for (const bool launch : {false, true}) {   // first every size, then every launch
+    if (launch && w.dry) break;
+    Work p = w;
+    p.dry = !launch;
+    if (launch) {
+      if (m > 0 && n > 0 && (want_dx || want_dw)) {
+        rc = quantize(st, dY, dy_fmt, pow2, 0, want_dx ? &dy1 : nullptr, want_dw ? &dy0 : nullptr);
+        if (rc) return rc;
+      }
+      if (m > 0 && k > 0 && want_dw) {
+        rc = quantize(st, X, x_fmt, pow2, 0, nullptr, &x0);
+        if (rc) return rc;
+      }
+    }
+    if (want_dx) {
+      rc = product(p, st, n, dy1, cols_of(*W, k), pow2, dx);
+      if (rc) return rc;
+    }
+    if (want_dw) {
+      rc = product(p, st, m, dy0, x0, pow2, dw);
+      if (rc) return rc;
+    }
+    if (!launch) {
+      if (w.dry)
+        w.used = p.used;
+      else if (p.used > w.bytes)
+        return OZFP4_EWORKSPACE;
+    }
+  }
+  return OZFP4_OK;
+}
+
+Work work_of(void* p, int64_t bytes) {
+  return {static_cast<uint8_t*>(p), p ? bytes : 0, 0, false};
+}
+bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 256 == 0; }
+
+// Outputs of the quantiser: lines along their unit stride.
+int check_quantized(const ozfp4_f8_matrix& M, int64_t line_stride, int64_t k_stride, int64_t k) {
+  if (!format_ok(M.format) || (M.tile != 0 && M.tile != 1) || !M.values || !M.scales) return OZFP4_EINVAL;
+  if (k_stride != 1 || line_stride < k || line_stride % 16 || reinterpret_cast<uintptr_t>(M.values) % 16)
+    return OZFP4_EINVAL;
+  if (M.srs < 0 || M.scs < 0) return OZFP4_EINVAL;
+  return OZFP4_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ozfp4_quantize_f8(int64_t rows, int64_t cols, const void* X, int x_type, int64_t x_rs, int64_t x_cs,
+                      int scale_type, const ozfp4_f8_matrix* along_cols, const ozfp4_f8_matrix* along_rows) {
+  if (!dims_ok(rows, cols, 0) || !tiles_ok(rows, cols, 128)) return OZFP4_EINVAL;
+  if (!type_ok(x_type) || !scale_ok(scale_type) || !layout_ok(rows, cols, x_rs, x_cs)) return OZFP4_EINVAL;
+  if (!along_cols && !along_rows) return OZFP4_EINVAL;
+  if (along_cols && along_rows &&
+      (along_cols->format != along_rows->format || along_cols->tile != along_rows->tile))
+    return OZFP4_EINVAL;
+  if (rows == 0 || cols == 0) return OZFP4_OK;
+  if (!X) return OZFP4_EINVAL;
+  Operand c, r;
+  if (along_cols) {
+    if (int rc = check_quantized(*along_cols, along_cols->rs, along_cols->cs, cols)) return rc;
+    c = rows_of(*along_cols, rows);
+  }
+  if (along_rows) {
+    if (int rc = check_quantized(*along_rows, along_rows->cs, along_rows->rs, rows)) return rc;
+    r = cols_of(*along_rows, cols);
+  }
+  const ozfp4_f8_matrix& any = along_cols ? *along_cols : *along_rows;
+  return quantize(library_stream(), Source{X, x_type, rows, cols, x_rs, x_cs}, any.format,
+                  scale_type == OZFP4_SCALE_E8M0, any.tile, along_cols ? &c : nullptr, along_rows ? &r : nullptr);
+}
+
+int ozfp4_gemm_f8(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A, const ozfp4_f8_matrix* B,
+                  int scale_type, void* C, int c_type, int64_t c_rs, int64_t c_cs, int accumulate,
+                  void* workspace, int64_t workspace_bytes) {
+  if (!scale_ok(scale_type) || !aligned(workspace)) return OZFP4_EINVAL;
+  Work w = work_of(workspace, workspace_bytes);
+  return gemm(w, m, n, k, A, B, scale_type == OZFP4_SCALE_E8M0, Out{C, c_type, c_rs, c_cs, accumulate != 0});
+}
+
+int ozfp4_gemm_f8_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A,
+                            const ozfp4_f8_matrix* B, int64_t c_rs, int64_t c_cs, int64_t* bytes) {
+  if (!bytes) return OZFP4_EINVAL;
+  Work w = {nullptr, 0, 0, true};
+  const int rc = gemm(w, m, n, k, A, B, 0, Out{nullptr, OZFP4_F32, c_rs, c_cs, 0});
+  *bytes = w.used;
+  return rc;
+}
+
+int ozfp4_linear_f8(int64_t m, int64_t n, int64_t k, const void* X, int x_type, int64_t x_rs, int64_t x_cs,
+                    int x_format, const ozfp4_f8_matrix* W, int scale_type, void* Y, int y_type, int64_t y_rs,
+                    int64_t y_cs, void* workspace, int64_t workspace_bytes) {
+  if (!scale_ok(scale_type) || !aligned(workspace)) return OZFP4_EINVAL;
+  Work w = work_of(workspace, workspace_bytes);
+  return linear(w, m, n, k, Source{X, x_type, m, k, x_rs, x_cs}, x_format, W, scale_type == OZFP4_SCALE_E8M0,
+                Out{Y, y_type, y_rs, y_cs, 0});
+}
+
+int ozfp4_linear_f8_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* W, int64_t y_rs,
+                              int64_t y_cs, int64_t* bytes) {
+  if (!bytes) return OZFP4_EINVAL;
+  Work w = {nullptr, 0, 0, true};
+  const int rc = linear(w, m, n, k, Source{}, OZFP4_E4M3, W, 0, Out{nullptr, OZFP4_F32, y_rs, y_cs, 0});
+  *bytes = w.used;
+  return rc;
+}
+
+int ozfp4_linear_f8_backward(int64_t m, int64_t n, int64_t k, const void* dY, int64_t dy_rs, int64_t dy_cs,
+                             int dy_format, const void* X, int64_t x_rs, int64_t x_cs, int x_format,
+                             int x_type, const ozfp4_f8_matrix* W, int scale_type, void* dX, int dx_type,
+                             int64_t dx_rs, int64_t dx_cs, float* dW, int64_t dw_rs, int64_t dw_cs,
+                             int accumulate, void* workspace, int64_t workspace_bytes) {
+  if (!scale_ok(scale_type) || !aligned(workspace)) return OZFP4_EINVAL;
+  Work w = work_of(workspace, workspace_bytes);
+  return backward(w, m, n, k, Source{dY, x_type, m, n, dy_rs, dy_cs}, dy_format, Source{X, x_type, m, k, x_rs, x_cs},
+                  x_format, W, scale_type == OZFP4_SCALE_E8M0, dX != nullptr, Out{dX, dx_type, dx_rs, dx_cs, 0},
+                  dW != nullptr, Out{dW, OZFP4_F32, dw_rs, dw_cs, accumulate != 0});
+}
+
+int ozfp4_linear_f8_backward_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* W,
+                                       int64_t dx_rs, int64_t dx_cs, int64_t dw_rs, int64_t dw_cs,
+                                       int64_t* bytes) {
+  if (!bytes) return OZFP4_EINVAL;
+  Work w = {nullptr, 0, 0, true};
+  const int rc = backward(w, m, n, k, Source{}, OZFP4_E4M3, Source{}, OZFP4_E4M3, W, 0, true,
+                          Out{nullptr, OZFP4_F32, dx_rs, dx_cs, 0}, true, Out{nullptr, OZFP4_F32, dw_rs, dw_cs, 0});
+  *bytes = w.used;
+  return rc;
+}
+
+}  // extern "C"

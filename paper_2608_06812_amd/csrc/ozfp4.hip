@@ -10,6 +10,7 @@
 
 #include "calibrate.hpp"
 #include "convert.hpp"
+#include "f8.hpp"
 #include "gemm_short.hpp"
 #include "igemm.hpp"
 #include "karatsuba.hpp"
@@ -1022,6 +1023,8 @@ int sgemm_moduli(int64_t k) {
 
 }  // namespace
 
+hipStream_t ozfp4::library_stream() { return g_stream; }
+
 extern "C" {
 
 int ozfp4_dgemm(int64_t m, int64_t n, int64_t k, const double* A, int64_t lda,
@@ -1179,6 +1182,7 @@ const char* ozfp4_strerror(int code) {
     case OZFP4_ESCRATCH:
       return "ozfp4_dgemm_noalloc: device not set up (call ozfp4_init), or the call needs more "
              "scratch than OZFP4_SCRATCH_BYTES";
+    case OZFP4_EWORKSPACE: return "the workspace of the call is too small";
     default: return "unknown error code";
   }
 }

@@ -32,6 +32,7 @@ OZFP4_ENONFINITE = -4
 OZFP4_ENOMEM = -5
 OZFP4_EHIP = -6
 OZFP4_ESCRATCH = -7
+OZFP4_EWORKSPACE = -8
 OZFP4_MIN_MODULI = 2
 OZFP4_MAX_MODULI = 27
 OZFP4_MAX_K = 131072
@@ -39,12 +40,26 @@ OZFP4_MAX_K_S8 = 16777216
 OZFP4_MAX_ELEMENTS = 1 << 48
 OZFP4_OZI_MAX_LIMBS = 15
 OZFP4_SCRATCH_BYTES = 268435456
+OZFP4_MAX_K_F8 = 4194304
+OZFP4_MAX_TILES_F8 = 16777215
+OZFP4_F32, OZFP4_BF16, OZFP4_F16 = range(3)
+OZFP4_E4M3, OZFP4_E5M2 = range(2)
+OZFP4_SCALE_F32, OZFP4_SCALE_E8M0 = range(2)
 (OZFP4_OP_DGEMM, OZFP4_OP_DGEMM_NOALLOC, OZFP4_OP_DGEMM_SPLIT, OZFP4_OP_DGEMM_OZI, OZFP4_OP_SGEMM,
  OZFP4_OP_IGEMM_S8) = range(6)
 
 _lib = None
 
 _i64, _int, _p = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p
+
+
+class F8Matrix(ctypes.Structure):
+    """ozfp4_f8_matrix: 8-bit values and their scales."""
+    _fields_ = [("values", _p), ("rs", _i64), ("cs", _i64), ("scales", _p), ("srs", _i64), ("scs", _i64),
+                ("format", ctypes.c_int32), ("tile", ctypes.c_int32)]
+
+
+_f8 = ctypes.POINTER(F8Matrix)
 _SIGNATURES = {
     "ozfp4_dgemm": (_int, [_i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _int]),
     "ozfp4_igemm_s8": (_int, [_i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64]),
@@ -52,6 +67,15 @@ _SIGNATURES = {
     "ozfp4_dgemm_split": (_int, [_i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _int]),
     "ozfp4_dgemm_noalloc": (_int, [_i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _int]),
     "ozfp4_product": (_int, [_int, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _p, _i64, _int]),
+    "ozfp4_quantize_f8": (_int, [_i64, _i64, _p, _int, _i64, _i64, _int, _f8, _f8]),
+    "ozfp4_gemm_f8": (_int, [_i64, _i64, _i64, _f8, _f8, _int, _p, _int, _i64, _i64, _int, _p, _i64]),
+    "ozfp4_gemm_f8_workspace": (_int, [_i64, _i64, _i64, _f8, _f8, _i64, _i64, _p]),
+    "ozfp4_linear_f8": (_int, [_i64, _i64, _i64, _p, _int, _i64, _i64, _int, _f8, _int, _p, _int, _i64, _i64,
+                               _p, _i64]),
+    "ozfp4_linear_f8_workspace": (_int, [_i64, _i64, _i64, _f8, _i64, _i64, _p]),
+    "ozfp4_linear_f8_backward": (_int, [_i64, _i64, _i64, _p, _i64, _i64, _int, _p, _i64, _i64, _int, _int, _f8,
+                                        _int, _p, _int, _i64, _i64, _p, _i64, _i64, _int, _p, _i64]),
+    "ozfp4_linear_f8_backward_workspace": (_int, [_i64, _i64, _i64, _f8, _i64, _i64, _i64, _i64, _p]),
     "ozfp4_set_stream": (_int, [_p]),
     "ozfp4_finalize": (_int, []),
     "ozfp4_strerror": (ctypes.c_char_p, [_int]),
@@ -127,6 +151,45 @@ def ozfp4_igemm_s8(m, n, k, A, lda, B, ldb, C, ldc) -> int:
 
 def ozfp4_product(op, m, n, k, A, a_rs, a_cs, B, b_rs, b_cs, C, ldc, count) -> int:
     return load().ozfp4_product(op, m, n, k, A, a_rs, a_cs, B, b_rs, b_cs, C, ldc, count)
+
+
+def ozfp4_quantize_f8(rows, cols, X, x_type, x_rs, x_cs, scale_type, along_cols, along_rows) -> int:
+    return load().ozfp4_quantize_f8(rows, cols, X, x_type, x_rs, x_cs, scale_type, along_cols, along_rows)
+
+
+def ozfp4_gemm_f8(m, n, k, A, B, scale_type, C, c_type, c_rs, c_cs, accumulate, workspace, nbytes) -> int:
+    return load().ozfp4_gemm_f8(m, n, k, A, B, scale_type, C, c_type, c_rs, c_cs, accumulate, workspace, nbytes)
+
+
+def ozfp4_gemm_f8_workspace(m, n, k, A, B, c_rs, c_cs) -> int:
+    out = ctypes.c_int64()
+    _check(load().ozfp4_gemm_f8_workspace(m, n, k, A, B, c_rs, c_cs, ctypes.byref(out)),
+           "ozfp4_gemm_f8_workspace")
+    return out.value
+
+
+def ozfp4_linear_f8(m, n, k, X, x_type, x_rs, x_cs, x_format, W, scale_type, Y, y_type, y_rs, y_cs, workspace,
+                    nbytes) -> int:
+    return load().ozfp4_linear_f8(m, n, k, X, x_type, x_rs, x_cs, x_format, W, scale_type, Y, y_type, y_rs, y_cs,
+                                  workspace, nbytes)
+
+
+def ozfp4_linear_f8_workspace(m, n, k, W, y_rs, y_cs) -> int:
+    out = ctypes.c_int64()
+    _check(load().ozfp4_linear_f8_workspace(m, n, k, W, y_rs, y_cs, ctypes.byref(out)),
+           "ozfp4_linear_f8_workspace")
+    return out.value
+
+
+def ozfp4_linear_f8_backward(*args) -> int:
+    return load().ozfp4_linear_f8_backward(*args)
+
+
+def ozfp4_linear_f8_backward_workspace(m, n, k, W, dx_rs, dx_cs, dw_rs, dw_cs) -> int:
+    out = ctypes.c_int64()
+    _check(load().ozfp4_linear_f8_backward_workspace(m, n, k, W, dx_rs, dx_cs, dw_rs, dw_cs, ctypes.byref(out)),
+           "ozfp4_linear_f8_backward_workspace")
+    return out.value
 
 
 def ozfp4_set_stream(stream) -> int:
@@ -509,6 +572,273 @@ def sgemm(A, B, n_moduli: int | None = None, out=None):
     # the error that any count below 2 is
     count = 0 if n_moduli is None else (n_moduli or 1)
     return _product(OZFP4_OP_SGEMM, A, B, torch.float32, torch.float32, count, out, "ozfp4_sgemm")
+
+
+# ----------------------- 8-bit products with a scale for each block of 128
+
+_f8_tables = None
+
+
+def _f8_types():
+    """Codes of (input and output types, 8-bit formats, scale types)."""
+    global _f8_tables
+    if _f8_tables is None:
+        t = _th()
+        _f8_tables = ({t.float32: OZFP4_F32, t.bfloat16: OZFP4_BF16, t.float16: OZFP4_F16},
+                      {t.float8_e4m3fn: OZFP4_E4M3, t.float8_e5m2: OZFP4_E5M2},
+                      {t.float32: OZFP4_SCALE_F32, t.float8_e8m0fnu: OZFP4_SCALE_E8M0})
+    return _f8_tables
+
+
+def _blocks(v):
+    return (v + 127) // 128
+
+
+def _code(table, dtype, what):
+    code = table.get(dtype)
+    if code is None:
+        raise TypeError(f"{what} must be one of {', '.join(str(d) for d in table)}")
+    return code
+
+
+def _device_matrix(X, name):
+    if not isinstance(X, _th().Tensor) or X.dim() != 2:
+        raise TypeError(f"{name} must be a 2-D torch tensor")
+    if not X.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+
+
+def _unit(X):
+    """(row stride, column stride) with one of them 1, or None if the tensor
+    has no such layout."""
+    r, c = X.shape
+    rs, cs = X.stride()
+    if r <= 1:
+        return (max(1, c), 1) if c <= 1 or cs == 1 else (1, cs) if cs > 0 else None
+    if c <= 1:
+        return (rs, 1) if rs > 0 else None
+    return (rs, cs) if (cs == 1 and rs >= c) or (rs == 1 and cs >= r) else None
+
+
+def _source(X, name):
+    """X with a unit stride (a row-major copy of any other layout), its type
+    code and its strides."""
+    _device_matrix(X, name)
+    code = _code(_f8_types()[0], X.dtype, name)
+    st = _unit(X)
+    if st is None:
+        X = X.contiguous()
+        st = _unit(X)
+    return X, code, st
+
+
+def _quantized(Q, S, axis, name):
+    """F8Matrix of values Q and scales S along `axis`, the scale code, and the
+    tensors that back it."""
+    _device_matrix(Q, name)
+    _device_matrix(S, "S" + name)
+    _, formats, scales = _f8_types()
+    fmt = _code(formats, Q.dtype, name)
+    kind = _code(scales, S.dtype, "S" + name)
+    r, c = Q.shape
+    lines = (_blocks(r), c) if axis == 0 else (r, _blocks(c))
+    tiles = (_blocks(r), _blocks(c))
+    shape = tuple(S.shape)
+    if shape != lines and shape != tiles:
+        raise ValueError(f"S{name} must have shape {lines} or {tiles}, not {shape}")
+    st = _unit(Q)
+    if st is None:
+        Q = Q.contiguous()
+        st = _unit(Q)
+    srs, scs = S.stride()
+    return F8Matrix(Q.data_ptr(), st[0], st[1], S.data_ptr(), srs, scs, fmt, shape != lines), kind, Q
+
+
+def _output(out, shape, dtype, device, name):
+    """`out` or a new row-major tensor, its type code and strides."""
+    code = _code(_f8_types()[0], dtype, f"{name}'s type")
+    if out is None:
+        C = _th().empty(shape, dtype=dtype, device=device)
+    else:
+        _device_matrix(out, name)
+        C = out
+        if tuple(C.shape) != tuple(shape) or C.dtype != dtype:
+            raise ValueError(f"{name} must be a {str(dtype).split('.')[-1]} tensor of shape {tuple(shape)}")
+    st = _unit(C)
+    if st is None:
+        raise ValueError(f"{name} must be row-major or column-major")
+    return C, code, st
+
+
+def _scratch(nbytes, device):
+    """(tensor, address) of a call's workspace. It comes from torch's
+    allocator: it belongs to the call's stream, or to the graph that the call
+    is captured into, and no two calls in flight share it."""
+    if nbytes == 0:
+        return None, None
+    T = _th().empty(nbytes, dtype=_th().uint8, device=device)
+    return T, T.data_ptr()
+
+
+def _run(device, tensors, call, where):
+    """The library call on `device` and its current stream (see _on)."""
+    torch, dev = _th(), device.index
+    if dev == torch.cuda.current_device() and all(T.get_device() == dev for T in tensors):
+        load().ozfp4_set_stream(torch.cuda.current_stream(dev).cuda_stream)
+        code = call()
+    else:
+        with _on(device, *tensors):
+            code = call()
+    _check(code, where)
+
+
+def _quantize_f8(X, dims, tile, format, scale):
+    torch = _th()
+    format = torch.float8_e4m3fn if format is None else format
+    scale = torch.float32 if scale is None else scale
+    _, formats, scales = _f8_types()
+    fmt, kind = _code(formats, format, "format"), _code(scales, scale, "scale")
+    X, code, (rs, cs) = _source(X, "X")
+    r, c = X.shape
+    out, mats = [], [None, None]
+    S = None
+    for dim in dims:
+        # lines of adjacent values, 16-byte aligned as the products read them,
+        # and scales with the lines adjacent
+        if dim == 1:
+            Q = torch.empty((r, (c + 15) // 16 * 16), dtype=format, device=X.device)[:, :c]
+        else:
+            Q = torch.empty((c, (r + 15) // 16 * 16), dtype=format, device=X.device)[:, :r].t()
+        if tile:
+            S = torch.empty((_blocks(r), _blocks(c)), dtype=scale, device=X.device) if S is None else S
+        elif dim == 1:
+            S = torch.empty((_blocks(c), r), dtype=scale, device=X.device).t()
+        else:
+            S = torch.empty((_blocks(r), c), dtype=scale, device=X.device)
+        pad = (c if dim == 1 else r) + 15 & ~15
+        strides = (max(16, pad), 1) if dim == 1 else (1, max(16, pad))
+        mats[dim] = F8Matrix(Q.data_ptr(), *strides, S.data_ptr(), *S.stride(), fmt, 1 if tile else 0)
+        out += [Q, S]
+    if r > 0 and c > 0:
+        _run(X.device, (X,), lambda: load().ozfp4_quantize_f8(r, c, X.data_ptr(), code, rs, cs, kind, mats[1], mats[0]),
+             "ozfp4_quantize_f8")
+    return out
+
+
+def quantize_f8(X, dim: int = 1, tile: bool = False, format=None, scale=None):
+    """8-bit values Q and scales S of a float32, bfloat16 or float16 device
+    tensor X (2-D), X ~ Q S, for a product that sums over dimension `dim`: one
+    scale per line of 128 elements along it, or with `tile` per 128 x 128
+    elements. format: torch.float8_e4m3fn (default) or torch.float8_e5m2;
+    scale: torch.float32 (default) or torch.float8_e8m0fnu, powers of two.
+    Scale and rounding as ozfp4_quantize_f8. Q has X's shape, with dimension
+    `dim` adjacent in memory; S has X's with `dim` (with `tile` both) divided
+    by 128 and rounded up."""
+    if dim not in (0, 1):
+        raise ValueError("dim must be 0 or 1")
+    return tuple(_quantize_f8(X, (dim,), tile, format, scale))
+
+
+def quantize_f8_both(X, tile: bool = False, format=None, scale=None):
+    """(Q1, S1, Q0, S0): quantize_f8 along dimension 1 and along dimension 0
+    from one read of X. With `tile`, S1 and S0 are one tensor."""
+    return tuple(_quantize_f8(X, (1, 0), tile, format, scale))
+
+
+def gemm_f8(A, SA, B, SB, out_dtype=None, out=None, accumulate: bool = False):
+    """C = (A SA)(B SB) for 8-bit device tensors A (m x k), B (k x n) in either
+    storage order with scales SA along dimension 1 of A and SB along dimension
+    0 of B, per line or per tile of 128 (their shapes tell which), both float32
+    or both float8_e8m0fnu; sums in FP32, rounded once to out_dtype (float32,
+    bfloat16 or float16; default bfloat16, or out's). accumulate: out (float32)
+    is added to. Returns C (m x n), `out` or a new row-major tensor. Operands
+    with k adjacent and lines 16-byte aligned, as quantize_f8 makes them, are
+    read in place. Asynchronous; can be captured into a graph."""
+    a, kind, A = _quantized(A, SA, 1, "A")
+    b, kind_b, B = _quantized(B, SB, 0, "B")
+    m, k = A.shape
+    k2, n = B.shape
+    if k != k2:
+        raise ValueError("inner dimensions differ")
+    if kind != kind_b:
+        raise TypeError("SA and SB must be of one type")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    if out_dtype is None:
+        out_dtype = _th().bfloat16 if out is None else out.dtype
+    C, code, (rs, cs) = _output(out, (m, n), out_dtype, A.device, "out")
+    if accumulate and code != OZFP4_F32:
+        raise TypeError("accumulate needs a float32 out")
+    ws, p = _scratch(ozfp4_gemm_f8_workspace(m, n, k, a, b, rs, cs), A.device)
+    _run(A.device, (A, SA, B, SB, C),
+         lambda: load().ozfp4_gemm_f8(m, n, k, a, b, kind, C.data_ptr(), code, rs, cs, 1 if accumulate else 0, p,
+                                      0 if ws is None else ws.numel()), "ozfp4_gemm_f8")
+    return C
+
+
+def linear_f8(X, W, SW, out_dtype=None, format=None, out=None):
+    """Y = Xq W^T for X (m x k, float32, bfloat16 or float16) quantised in the
+    call as by quantize_f8(X, 1, format=format) with scales of SW's type, and
+    weights W (n x k) with scales SW along dimension 1. out_dtype defaults to
+    X's type (or out's). Returns Y (m x n), `out` or a new row-major tensor.
+    Asynchronous; can be captured into a graph."""
+    torch = _th()
+    w, kind, W = _quantized(W, SW, 1, "W")
+    fmt = _code(_f8_types()[1], torch.float8_e4m3fn if format is None else format, "format")
+    X, x_code, (x_rs, x_cs) = _source(X, "X")
+    m, k = X.shape
+    n, k2 = W.shape
+    if k != k2:
+        raise ValueError("inner dimensions differ")
+    if out_dtype is None:
+        out_dtype = X.dtype if out is None else out.dtype
+    Y, code, (rs, cs) = _output(out, (m, n), out_dtype, X.device, "out")
+    ws, p = _scratch(ozfp4_linear_f8_workspace(m, n, k, w, rs, cs), X.device)
+    _run(X.device, (X, W, SW, Y),
+         lambda: load().ozfp4_linear_f8(m, n, k, X.data_ptr(), x_code, x_rs, x_cs, fmt, w, kind, Y.data_ptr(), code, rs,
+                                        cs, p, 0 if ws is None else ws.numel()), "ozfp4_linear_f8")
+    return Y
+
+
+def linear_f8_backward(dY, X, W, SW, format=None, out_dtype=None, dX=None, dW=None, accumulate: bool = False,
+                       x_format=None):
+    """(dX, dW) of linear_f8 for the output gradient dY (m x n, of X's type):
+    dX = dYq W with dY quantised along dimension 1, dW = dYq^T Xq with dY and X
+    quantised along dimension 0; `format` (default float8_e4m3fn) is dY's,
+    x_format X's. W is tile-scaled: SW has a scale per 128 x 128. dX (m x k) of
+    out_dtype (default X's type, or dX's), dW (n x k) float32; accumulate: dW
+    is added to. Given tensors are written, others are new and row-major.
+    Asynchronous; can be captured into a graph."""
+    torch = _th()
+    e4m3 = torch.float8_e4m3fn
+    formats = _f8_types()[1]
+    fmt = _code(formats, e4m3 if format is None else format, "format")
+    x_fmt = _code(formats, e4m3 if x_format is None else x_format, "x_format")
+    w, kind, W = _quantized(W, SW, 1, "W")
+    dY, y_code, (y_rs, y_cs) = _source(dY, "dY")
+    X, x_code, (x_rs, x_cs) = _source(X, "X")
+    n, k = W.shape
+    m = X.shape[0]
+    if X.shape[1] != k or tuple(dY.shape) != (m, n):
+        raise ValueError("dY (m x n), X (m x k) and W (n x k) do not fit together")
+    if x_code != y_code:
+        raise TypeError("dY and X must be of one type")
+    if tuple(SW.shape) != (_blocks(n), _blocks(k)):
+        raise ValueError("SW must have a scale per 128 x 128 tile")
+    if accumulate and dW is None:
+        raise ValueError("accumulate needs dW")
+    if out_dtype is None:
+        out_dtype = X.dtype if dX is None else dX.dtype
+    dX, code, (dx_rs, dx_cs) = _output(dX, (m, k), out_dtype, X.device, "dX")
+    dW, _, (dw_rs, dw_cs) = _output(dW, (n, k), torch.float32, X.device, "dW")
+    w.tile = 1
+    ws, p = _scratch(ozfp4_linear_f8_backward_workspace(m, n, k, w, dx_rs, dx_cs, dw_rs, dw_cs), X.device)
+    _run(X.device, (dY, X, W, SW, dX, dW),
+         lambda: load().ozfp4_linear_f8_backward(
+             m, n, k, dY.data_ptr(), y_rs, y_cs, fmt, X.data_ptr(), x_rs, x_cs, x_fmt, x_code, w, kind,
+             dX.data_ptr(), code, dx_rs, dx_cs, dW.data_ptr(), dw_rs, dw_cs, 1 if accumulate else 0, p,
+             0 if ws is None else ws.numel()), "ozfp4_linear_f8_backward")
+    return dX, dW
 
 
 # ------------------------------------------------------- reference measurements
