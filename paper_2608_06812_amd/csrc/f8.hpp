@@ -47,16 +47,23 @@ struct F8Gemm {
 
 hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g);
 
-// Sum of `ranges` partial products (q * ldp + p, part elements apart) into C.
-struct F8Sum {
-  const float* x;
-  int64_t ldp, part, lines_p, lines_q;
-  int ranges;
+// The same with few lines of Q; element (p, q) at C[p * cp + q * cq]. Lines of
+// any alignment. x (or null): the lines of Q as they are, value kk of line i
+// at x[i * ldx + kk], quantised in the kernel to Q.fmt.
+constexpr int kF8TokenLines = 64;     // lines of Q, at most; with x 16
+constexpr int64_t kF8TokenMany = 1 << 26;   // lines of P, at most (one launch)
+constexpr int kF8TokenBlocks = 256;   // with x: lines times blocks of 128, at most
+struct F8Token {
+  F8Lines P, Q;
+  int64_t k;
   void* C;
-  int64_t ldc;
-  int type, accumulate;
+  int64_t cp, cq;
+  int type, accumulate, pow2;
+  const void* x;
+  int64_t ldx;
+  int src;
 };
-hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s);
+hipError_t launch_f8_token(hipStream_t st, const F8Token& t);
 
 // Bytes (line, kk) at x[line * ls + kk * ks], one stride 1, to lines of k
 // adjacent bytes with line stride ld (a multiple of 16).

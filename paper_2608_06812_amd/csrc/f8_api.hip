@@ -94,17 +94,41 @@ int check_out(const Out& c, int64_t rows, int64_t cols) {
   return OZFP4_OK;
 }
 
+F8Token token_product(int64_t k, const Operand& few, const Operand& many, bool few_rows, int pow2, const Out& c) {
+  F8Token t = {};
+  t.P = many.l;
+  t.Q = few.l;
+  t.k = k;
+  t.C = c.C;
+  t.cp = few_rows ? c.cs : c.rs;
+  t.cq = few_rows ? c.rs : c.cs;
+  t.type = c.type;
+  t.accumulate = c.accumulate;
+  t.pow2 = pow2;
+  return t;
+}
+
 // C = A B from the rows of A and the columns of B.
 int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, const Out& c) {
   if (A.l.lines == 0 || B.l.lines == 0 || (k == 0 && c.accumulate)) return OZFP4_OK;
+  const bool few_rows = A.l.lines <= B.l.lines;
+  const bool tokens = k > 0 && std::min(A.l.lines, B.l.lines) <= kF8TokenLines &&
+                      std::max(A.l.lines, B.l.lines) <= kF8TokenMany;
   F8Pack pack[2];
   int packs = 0;
   for (Operand* o : {&A, &B}) {
-    if (k == 0 || in_place(*o, k)) continue;
+    if (k == 0 || in_place(*o, k) || (tokens && (o->ks == 1 || k == 1))) continue;
     const int64_t ld = round_up(k, 128);
     pack[packs++] = {o->l.x, o->l.ld, o->ks, o->l.lines, k, w.take(o->l.lines * ld), ld};
     o->l.x = pack[packs - 1].out;
     o->l.ld = ld;
+  }
+  if (tokens) {
+    if (!w.fits()) return OZFP4_EWORKSPACE;
+    if (w.dry) return OZFP4_OK;
+    if (packs) F8_LAUNCH(launch_f8_pack(st, pack, packs));
+    F8_LAUNCH(launch_f8_token(st, token_product(k, few_rows ? A : B, few_rows ? B : A, few_rows, pow2, c)));
+    return OZFP4_OK;
   }
   F8Gemm g = {};
   // the lines of the operand along which C is adjacent are the kernel's P
@@ -206,17 +230,30 @@ int linear(Work& w, int64_t m, int64_t n, int64_t k, const Source& X, int fmt, c
     if (m > 0 && ((k > 0 && !X.x) || (n > 0 && !y.C))) return OZFP4_EINVAL;
   }
   if (m == 0 || n == 0) return OZFP4_OK;
+  const Operand weights = rows_of(*W, n);
+  if (m <= 16 && k > 0 && m * blocks_of(k) <= kF8TokenBlocks && n >= m && n <= kF8TokenMany && X.cs == 1 && (weights.ks == 1 || k == 1)) {
+    if (w.dry) return OZFP4_OK;
+    Operand x = {};
+    x.l.lines = m;
+    x.l.fmt = fmt;
+    F8Token t = token_product(k, x, weights, true, pow2, y);
+    t.x = X.x;
+    t.ldx = X.rs;
+    t.src = X.type;
+    F8_LAUNCH(launch_f8_token(library_stream(), t));
+    return OZFP4_OK;
+  }
   const Operand x = take_lines(w, m, k, fmt, pow2);
   if (!w.dry) {
     Work rest = w;   // nothing is launched in a workspace that is too small
     rest.dry = true;
-    rc = product(rest, nullptr, k, x, rows_of(*W, n), pow2, y);
+    rc = product(rest, nullptr, k, x, weights, pow2, y);
     if (rc) return rc;
     if (rest.used > w.bytes) return OZFP4_EWORKSPACE;
     rc = quantize(library_stream(), X, fmt, pow2, 0, &x, nullptr);
     if (rc) return rc;
   }
-  return product(w, library_stream(), k, x, rows_of(*W, n), pow2, y);
+  return product(w, library_stream(), k, x, weights, pow2, y);
 }
 
 int backward(Work& w, int64_t m, int64_t n, int64_t k, const Source& dY, int dy_fmt, const Source& X, int x_fmt,
@@ -345,7 +382,7 @@ int ozfp4_linear_f8_workspace(int64_t m, int64_t n, int64_t k, const ozfp4_f8_ma
                               int64_t y_cs, int64_t* bytes) {
   if (!bytes) return OZFP4_EINVAL;
   Work w = {nullptr, 0, 0, true};
-  const int rc = linear(w, m, n, k, Source{}, OZFP4_E4M3, W, 0, Out{nullptr, OZFP4_F32, y_rs, y_cs, 0});
+  const int rc = linear(w, m, n, k, Source{nullptr, 0, m, k, 1, 0}, OZFP4_E4M3, W, 0, Out{nullptr, OZFP4_F32, y_rs, y_cs, 0});
   *bytes = w.used;
   return rc;
 }

@@ -11,107 +11,10 @@
 // One block of 256 threads takes 128 x 128 elements of X, held in registers
 // from one read of X, whichever of the two directions are wanted. Memory
 // bound: the bytes are X once and each output once.
-#include "f8.hpp"
-#include "ozfp4.h"
+#include "f8_round.hpp"
 
 namespace ozfp4 {
 namespace {
-
-template <int kSrc> struct Source;
-template <> struct Source<OZFP4_F32> { typedef float T; };
-template <> struct Source<OZFP4_BF16> { typedef uint16_t T; };
-template <> struct Source<OZFP4_F16> { typedef _Float16 T; };
-
-__device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ float widen(_Float16 v) { return (float)v; }
-
-// |x| where it is finite, else 0
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = __builtin_fabsf(x);
-  return a < __builtin_inff() ? a : 0.0f;
-}
-
-// A block's scale and what its elements need: S = m 2^e, m in [1, 2), and
-// r = fl(1 / m).
-struct Scale {
-  float m, r;
-  int e;
-};
-
-template <int kFmt>
-__device__ __forceinline__ float scale_f32(float a) {
-  constexpr float top = kFmt == OZFP4_E4M3 ? 448.0f : 57344.0f;
-  return a == 0.0f ? 1.0f : __builtin_fmaxf(a / top, 1.1754943508222875e-38f);
-}
-
-// Exponent E of the power-of-two scale: t = 1.75 2^8 or 1.75 2^15, so for a =
-// f 2^e (f in [1, 2)) E = e - 8 (15), one more where f > 1.75. A subnormal a
-// gives -126 like every a below 2^-118.
-template <int kFmt>
-__device__ __forceinline__ int scale_exp(float a) {
-  const uint32_t b = __float_as_uint(a);
-  const int e = (int)(b >> 23) - 127 - (kFmt == OZFP4_E4M3 ? 8 : 15) + ((b & 0x7fffff) > 0x600000);
-  return a == 0.0f ? 0 : max(e, -126);
-}
-
-template <bool kPow2, int kFmt>
-__device__ __forceinline__ Scale make_scale(float a) {
-  Scale s;
-  if constexpr (kPow2) {
-    s.m = s.r = 1.0f;
-    s.e = scale_exp<kFmt>(a);
-  } else {
-    const uint32_t b = __float_as_uint(scale_f32<kFmt>(a));
-    s.e = (int)(b >> 23) - 127;
-    s.m = __uint_as_float((b & 0x7fffff) | 0x3f800000);
-    s.r = 1.0f / s.m;
-  }
-  return s;
-}
-
-template <bool kPow2, int kFmt>
-__device__ __forceinline__ void store_scale(void* s, int64_t at, float a) {
-  if constexpr (kPow2)
-    static_cast<uint8_t*>(s)[at] = (uint8_t)(scale_exp<kFmt>(a) + 127);
-  else
-    static_cast<float*>(s)[at] = scale_f32<kFmt>(a);
-}
-
-// x / S as an FP32 value that rounds to the format as the exact quotient
-// does. The FP32 quotient alone does not: a border between two 8-bit values
-// is itself an FP32 value, and quotients within 2^-25 of it fall on it. So
-// the quotient is rounded to odd: h is within an ulp, the exact residual x -
-// h S says on which side, and an even h (borders are even) that is not exact
-// moves one unit towards the quotient. Dividing x and S by 2^e first keeps the
-// residuals away from underflow for every x that does not round to zero.
-template <bool kPow2>
-__device__ __forceinline__ float quotient(float x, const Scale& s) {
-  const float y = __builtin_ldexpf(x, -s.e);
-  if constexpr (kPow2) return y;
-  const float q = y * s.r;
-  const float h = __builtin_fmaf(__builtin_fmaf(-q, s.m, y), s.r, q);
-  const float d = __builtin_fmaf(-h, s.m, y);
-  const uint32_t b = __float_as_uint(h);
-  const int step = 1 | ((int)(b ^ __float_as_uint(d)) >> 31);   // +1 away from zero
-  const bool move = d != 0.0f && !(b & 1);
-  const float v = __uint_as_float(move ? b + (uint32_t)step : b);
-  // NaN and infinities as they are; the residuals lose the sign of a zero
-  return __builtin_fabsf(x) < __builtin_inff() ? __builtin_copysignf(v, x) : x;
-}
-
-template <int kFmt>
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-  int v = 0;
-  if constexpr (kFmt == OZFP4_E4M3) {
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
-  } else {
-    v = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, v, false);
-    v = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, v, true);
-  }
-  return (uint32_t)v;
-}
 
 constexpr int kTLd = 128 + 8;   // bytes from column to column of the transposed tile in LDS
 

@@ -219,7 +219,8 @@ def check_gemm(lib, ops, out_dtype=torch.float32, out=None, accumulate=False):
 
 SIZES = [(1, 1, 1), (1, 128, 128), (2, 3, 5), (16, 16, 128), (17, 33, 129), (64, 64, 256), (65, 130, 384),
          (100, 1, 300), (1, 100, 300), (128, 128, 15), (256, 256, 512), (257, 255, 640), (300, 500, 1000),
-         (48, 700, 144), (513, 129, 131), (40, 1040, 1300)]
+         (48, 700, 144), (513, 129, 131), (40, 1040, 1300), (2, 5000, 1024),
+         (5000, 30, 1111), (64, 3000, 2048)]
 
 
 @pytest.mark.parametrize("kind", [F32, E8])
@@ -227,6 +228,23 @@ SIZES = [(1, 1, 1), (1, 128, 128), (2, 3, 5), (16, 16, 128), (17, 33, 129), (64,
 def test_gemm_sizes(gpu_lib, size, kind):
     for a_tile, b_tile in ((False, True), (False, False), (True, True), (True, False)):
         check_gemm(gpu_lib, operands(*size, kind, a_tile=a_tile, b_tile=b_tile))
+
+
+@pytest.mark.parametrize("kind", [F32, E8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gemm_large(gpu_lib, dtype, kind):
+    """Enough tiles for the large block tile, ragged ones among them."""
+    for m, n, k in ((3500, 3601, 300), (3585, 3590, 128), (4096, 3592, 515)):
+        for a_tile, b_tile in ((False, True), (False, False), (True, False)):
+            check_gemm(gpu_lib, operands(m, n, k, kind, E5, E4, a_tile, b_tile), dtype)
+    room = torch.full((3503, 3611), 7.0, device="cuda", dtype=dtype)
+    check_gemm(gpu_lib, operands(3500, 3601, 300, kind), dtype, out=room[1:3501, :3601])
+    room[1:3501, :3601] = 7.0
+    assert (room == 7.0).all()
+    ops = operands(3500, 3600, 1000, kind, b_tile=False)
+    first = gpu_lib.gemm_f8(*ops, dtype)
+    for _ in range(3):
+        assert torch.equal(first, gpu_lib.gemm_f8(*ops, dtype))
 
 
 @pytest.mark.parametrize("kind", [F32, E8])
