@@ -7,9 +7,14 @@
 // chip has work from a few thousand lines on. Their sums meet in LDS at the end,
 // in a fixed order.
 //
+// The values go to BF16 in registers whatever the output's type: the matrix
+// cores have nothing to wait for here, and the formats need no variants.
+//
 // For up to 16 tokens of few values the product can take the tokens as they
 // are (bfloat16, float16, float32): every block quantises all of them for
 // itself, into LDS, while its first weights are on their way.
+#include <type_traits>
+
 #include "f8_device.hpp"
 #include "f8_round.hpp"
 
@@ -53,150 +58,210 @@ __device__ __forceinline__ uint32_t load_scale(const F8Lines& l, int64_t line, i
   return static_cast<const uint32_t*>(l.s)[at];
 }
 
-// Element (row, col) of the tokens as they come.
-template <int kSrc>
-__device__ __forceinline__ float source_at(const F8Token& t, int64_t row, int64_t col) {
-  return widen(static_cast<const typename Source<kSrc>::T*>(t.x)[row * t.ldx + col]);
+__device__ __forceinline__ Frag<true> to_bf16(v8i w, uint32_t e8, int fmt) {
+  return fmt == OZFP4_E4M3 ? Frag<true>::make<OZFP4_E4M3>(w, e8) : Frag<true>::make<OZFP4_E5M2>(w, e8);
 }
 
-template <bool kExact, int kMode, int FP, int FQ, int TQ, int kSrc>
-__global__ __launch_bounds__(kTokWaves * 64, 4) void k_f8_token(F8Token t) {
-  constexpr bool kFused = kSrc >= 0, kPow = kMode == kPow2;
-  constexpr int kDeep = TQ <= 2 ? 4 : 2;              // blocks of 128 in flight in a wave
-  constexpr int kSum = kTokWaves * 256 * TQ * 4;
-  constexpr int kHold = kFused ? kF8TokenBlocks * (128 + 4) : 0;
+// The tokens, quantised into LDS: block b of token i at u = b m + i, 128 bytes
+// whose 16-byte piece c lies at c ^ (i % 8), and its scale behind them all.
+// Sixteen lanes a block of 128, eight values a lane.
+template <bool kPow, int kFmt, int kSrc>
+__device__ __forceinline__ void quantize_tokens(const F8Token& t, int m, int total, uint8_t* lds, uint32_t* scales) {
+  typedef typename Source<kSrc>::T T;
+  const int tid = threadIdx.x, r = tid & 15, count = m * total;
+  for (int u = tid >> 4; u < count; u += kTokWaves * 4) {
+    const int b = u / m, i = u - b * m;
+    const int64_t col = (int64_t)b * kF8Block + r * 8;
+    const T* src = static_cast<const T*>(t.x) + i * t.ldx + col;
+    float x[8], a = 0.0f;
+    if (col + 8 <= t.k) {
+      T v[8];
+      __builtin_memcpy(v, src, sizeof(v));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = widen(v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = col + e < t.k ? widen(src[e]) : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a = __builtin_fmaxf(a, finite_abs(x[e]));
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
+    const Scale s = make_scale<kPow, kFmt>(a);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = quotient<kPow>(x[e], s);
+    *reinterpret_cast<uint2*>(lds + u * 128 + (((r >> 1) ^ (i & 7)) * 16) + (r & 1) * 8) =
+        uint2{pack4<kFmt>(x[0], x[1], x[2], x[3]), pack4<kFmt>(x[4], x[5], x[6], x[7])};
+    if (r == 0) {
+      if constexpr (kPow)
+        scales[u] = (uint32_t)(scale_exp<kFmt>(a) + 127);
+      else
+        scales[u] = __float_as_uint(scale_f32<kFmt>(a));
+    }
+  }
+}
+
+// A block: 16 TP lines of P, all lines of Q (16 TQ at most). The tokens are
+// the rows of the matrix instruction and the lines of P its columns, so that a
+// lane needs one scale of P a tile, whether that is a line's or a tile's.
+template <bool kPow, int TP, int TQ, int kSrc>
+__global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_token(F8Token t) {
+  constexpr bool kFused = kSrc >= 0;
+  constexpr int kDeep = 2;              // blocks of 128 in flight in a wave
+  constexpr int kOut = 256 * TP * TQ;
+  constexpr int kSum = kTokWaves * kOut * 4, kHold = kFused ? kF8TokenBlocks * (128 + 4) : 0;
   __shared__ __align__(16) uint8_t lds[kSum > kHold ? kSum : kHold];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int64_t p0 = (int64_t)blockIdx.x * 16;
+  const int64_t p0 = (int64_t)blockIdx.x * (16 * TP);
   const int total = (int)((t.k + kF8Block - 1) / kF8Block);
   const int tail = (int)(t.k - (int64_t)(total - 1) * kF8Block);
   const int m = (int)t.Q.lines;
+  uint32_t* held = reinterpret_cast<uint32_t*>(lds + kF8TokenBlocks * 128);
 
-  const uint8_t* px = t.P.x + min(p0 + r, t.P.lines - 1) * t.P.ld;
+  // this lane's lines; those behind the last are read as the last
+  int64_t lp[TP];
+  const uint8_t* px[TP];
+#pragma unroll
+  for (int i = 0; i < TP; ++i) {
+    lp[i] = min(p0 + i * 16 + r, t.P.lines - 1);
+    px[i] = t.P.x + lp[i] * t.P.ld;
+  }
+  int lq[TQ];
   const uint8_t* qx[TQ];
 #pragma unroll
-  for (int j = 0; j < TQ; ++j) qx[j] = t.Q.x + (int64_t)min(j * 16 + r, m - 1) * t.Q.ld;
+  for (int j = 0; j < TQ; ++j) {
+    lq[j] = min(j * 16 + r, m - 1);
+    qx[j] = t.Q.x + lq[j] * t.Q.ld;
+  }
 
   struct Stage {
-    v8i p;
-    uint32_t sp[kMode == kLineP ? 4 : 1];
+    v8i p[TP], q[TQ];
+    uint32_t sp[TP], sq[TQ];
   };
-  auto fetch = [&](int s) {
-    Stage f;
-    const uint8_t* at = px + (int64_t)s * kF8Block;
-    if (s == total - 1 && tail < kF8Block)
-      f.p = load_block<false>(at, g, tail);
-    else
-      f.p = load_block<true>(at, g, kF8Block);
-    if constexpr (kMode == kLineP) {
+  auto fetch = [&](int s, Stage& f) {
+    const int64_t at = (int64_t)s * kF8Block;
+    auto blocks = [&](auto whole, int left) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) f.sp[v] = load_scale<false>(t.P, min(p0 + g * 4 + v, t.P.lines - 1), s);
-    } else {
-      f.sp[0] = load_scale<kPow>(t.P, min(p0 + (kPow ? r : 0), t.P.lines - 1), s);
+      for (int i = 0; i < TP; ++i) f.p[i] = load_block<decltype(whole)::value>(px[i] + at, g, left);
+      if constexpr (!kFused) {
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) f.q[j] = load_block<decltype(whole)::value>(qx[j] + at, g, left);
+      }
+    };
+    if (s == total - 1 && tail < kF8Block)
+      blocks(std::false_type{}, tail);
+    else
+      blocks(std::true_type{}, kF8Block);
+#pragma unroll
+    for (int i = 0; i < TP; ++i) f.sp[i] = load_scale<kPow>(t.P, lp[i], s);
+    if constexpr (!kFused) {
+#pragma unroll
+      for (int j = 0; j < TQ; ++j) f.sq[j] = load_scale<kPow>(t.Q, lq[j], s);
     }
-    return f;
   };
 
   Stage st[kDeep];
 #pragma unroll
   for (int d = 0; d < kDeep; ++d)
-    if (wave + d * kTokWaves < total) st[d] = fetch(wave + d * kTokWaves);
+    if (wave + d * kTokWaves < total) fetch(wave + d * kTokWaves, st[d]);
 
-  float* held_scale = reinterpret_cast<float*>(lds + kF8TokenBlocks * 128);
   if constexpr (kFused) {
-    // sixteen lanes a block of 128, eight values a lane; block b of token i at
-    // (b m + i), its piece c at c ^ (i % 8)
-    const int count = m * total;
-    for (int u = tid >> 4; u < count; u += kTokWaves * 4) {
-      const int b = u / m, i = u - b * m, c0 = r * 8;
-      const int64_t col = (int64_t)b * kF8Block + c0;
-      float x[8], a = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = col + e < t.k ? source_at<kSrc>(t, i, col + e) : 0.0f;
-        a = __builtin_fmaxf(a, finite_abs(x[e]));
-      }
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
-      const Scale s = make_scale<kPow, FQ>(a);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = quotient<kPow>(x[e], s);
-      *reinterpret_cast<uint2*>(lds + u * 128 + (((r >> 1) ^ (i & 7)) * 16) + (r & 1) * 8) =
-          uint2{pack4<FQ>(x[0], x[1], x[2], x[3]), pack4<FQ>(x[4], x[5], x[6], x[7])};
-      if (r == 0) {
-        if constexpr (kPow)
-          reinterpret_cast<uint32_t*>(held_scale)[u] = (uint32_t)(scale_exp<FQ>(a) + 127);
-        else
-          held_scale[u] = scale_f32<FQ>(a);
-      }
-    }
+    if (t.Q.fmt == OZFP4_E4M3)
+      quantize_tokens<kPow, OZFP4_E4M3, kSrc>(t, m, total, lds, held);
+    else
+      quantize_tokens<kPow, OZFP4_E5M2, kSrc>(t, m, total, lds, held);
     __syncthreads();
   }
 
-  v4f acc[TQ];
+  v4f acc[TP][TQ];
 #pragma unroll
-  for (int j = 0; j < TQ; ++j) acc[j] = v4f{0, 0, 0, 0};
-  constexpr uint32_t one = 127;
+  for (int i = 0; i < TP; ++i)
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+  constexpr uint32_t one = 127;   // E8M0 1
 
   for (int s0 = wave; s0 < total; s0 += kTokWaves * kDeep) {
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) {
       const int s = s0 + d * kTokWaves;
       if (s >= total) break;
-      const Stage f = st[d];
-      v8i q[TQ];
-      uint32_t sq[TQ];
+      Stage& f = st[d];
+      if constexpr (kFused) {
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) {
-        const int i = min(j * 16 + r, m - 1);
-        if constexpr (kFused) {
-          const uint8_t* b = lds + (s * m + i) * 128;
-          const v4i x = *reinterpret_cast<const v4i*>(b + ((g ^ (i & 7)) * 16));
-          const v4i y = *reinterpret_cast<const v4i*>(b + (((g + 4) ^ (i & 7)) * 16));
-          q[j] = v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-          sq[j] = reinterpret_cast<const uint32_t*>(held_scale)[s * m + i];
-        } else {
-          const uint8_t* at = qx[j] + (int64_t)s * kF8Block;
-          if (s == total - 1 && tail < kF8Block)
-            q[j] = load_block<false>(at, g, tail);
-          else
-            q[j] = load_block<true>(at, g, kF8Block);
-          sq[j] = load_scale<kPow>(t.Q, i, s);
+        for (int j = 0; j < TQ; ++j) {
+          const uint8_t* b = lds + (s * m + lq[j]) * 128;
+          const v4i x = *reinterpret_cast<const v4i*>(b + ((g ^ (lq[j] & 7)) * 16));
+          const v4i y = *reinterpret_cast<const v4i*>(b + (((g + 4) ^ (lq[j] & 7)) * 16));
+          f.q[j] = v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+          f.sq[j] = held[s * m + lq[j]];
         }
       }
-      if (s + kTokWaves * kDeep < total) st[d] = fetch(s + kTokWaves * kDeep);
-      const auto p = Frag<kExact>::template make<FP>(f.p, kPow ? f.sp[0] : one);
+      float sq[TQ][4];   // scales of this lane's rows, tokens 4 g .. + 3
+      if constexpr (!kPow) {
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) {
-        const auto qf = Frag<kExact>::template make<FQ>(q[j], kPow ? sq[j] : one);
+        for (int j = 0; j < TQ; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sq[j][v] = __shfl(__uint_as_float(f.sq[j]), g * 4 + v);
+      }
+      auto as_p = [&](int i) { return to_bf16(f.p[i], kPow ? f.sp[i] : one, t.P.fmt); };
+      auto as_q = [&](int j) { return to_bf16(f.q[j], kPow ? f.sq[j] : one, t.Q.fmt); };
+      auto add = [&](int i, int j, const Frag<true>& p, const Frag<true>& q) {
         if constexpr (kPow) {
-          acc[j] = block_product<true, FP, FQ>(p, qf, acc[j], f.sp[0], sq[j]);
+          acc[i][j] = block_product<true, 0, 0>(q, p, acc[i][j], 0, 0);
         } else {
-          const v4f c = block_product<false, FP, FQ>(p, qf, v4f{0, 0, 0, 0}, 0, 0);
-          const float b = __uint_as_float(sq[j]);
+          const v4f c = block_product<false, 0, 0>(q, p, v4f{0, 0, 0, 0}, 0, 0);
 #pragma unroll
           for (int v = 0; v < 4; ++v)
-            acc[j][v] = __builtin_fmaf(c[v], __uint_as_float(f.sp[kMode == kLineP ? v : 0]) * b, acc[j][v]);
+            acc[i][j][v] = __builtin_fmaf(c[v], sq[j][v] * __uint_as_float(f.sp[i]), acc[i][j][v]);
+        }
+      };
+      // the fewer operands stay converted, the others pass one by one
+      if constexpr (TP <= TQ) {
+        Frag<true> p[TP];
+#pragma unroll
+        for (int i = 0; i < TP; ++i) p[i] = as_p(i);
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+          const Frag<true> q = as_q(j);
+#pragma unroll
+          for (int i = 0; i < TP; ++i) add(i, j, p[i], q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+        Frag<true> q[TQ];
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) q[j] = as_q(j);
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+          const Frag<true> p = as_p(i);
+#pragma unroll
+          for (int j = 0; j < TQ; ++j) add(i, j, p, q[j]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
+      if (s + kTokWaves * kDeep < total) fetch(s + kTokWaves * kDeep, f);
     }
   }
 
-  // the waves' sums, wave by wave: element (token, line) at token 16 + line
+  // the waves' sums, wave by wave: element (token, line) at token 16 TP + line
   if constexpr (kFused) __syncthreads();
   float* sum = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int j = 0; j < TQ; ++j)
-    *reinterpret_cast<v4f*>(sum + wave * 256 * TQ + (j * 16 + r) * 16 + g * 4) = acc[j];
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+        sum[wave * kOut + (j * 16 + g * 4 + v) * (16 * TP) + i * 16 + r] = acc[i][j][v];
   __syncthreads();
-  for (int e = tid; e < 256 * TQ; e += kTokWaves * 64) {
-    const int64_t q = e >> 4, p = p0 + (e & 15);
+  for (int e = tid; e < kOut; e += kTokWaves * 64) {
+    const int64_t q = e / (16 * TP), p = p0 + e % (16 * TP);
     if (q >= m || p >= t.P.lines) continue;
     float v = sum[e];
 #pragma unroll
-    for (int w = 1; w < kTokWaves; ++w) v += sum[w * 256 * TQ + e];
+    for (int w = 1; w < kTokWaves; ++w) v += sum[w * kOut + e];
     const int64_t at = p * t.cp + q * t.cq;
     if (t.type == OZFP4_F32) {
       float* c = static_cast<float*>(t.C) + at;
@@ -209,48 +274,42 @@ __global__ __launch_bounds__(kTokWaves * 64, 4) void k_f8_token(F8Token t) {
   }
 }
 
-template <bool kExact, int kMode, int FP, int FQ, int TQ, int kSrc>
+template <bool kPow, int TP, int TQ, int kSrc>
 hipError_t launch(hipStream_t st, const F8Token& t) {
-  hipLaunchKernelGGL((k_f8_token<kExact, kMode, FP, FQ, TQ, kSrc>), dim3((unsigned)((t.P.lines + 15) / 16)),
+  hipLaunchKernelGGL((k_f8_token<kPow, TP, TQ, kSrc>), dim3((unsigned)((t.P.lines + 16 * TP - 1) / (16 * TP))),
                      dim3(kTokWaves * 64), 0, st, t);
   return hipGetLastError();
 }
 
-template <bool kExact, int kMode, int FP, int FQ>
+// Lines of P a block takes: as many as leave about a block a CU, since every
+// block reads all lines of Q.
+template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
+  if constexpr (TQ == 2) {
+    if (t.P.lines >= 4 * 16 * 256) return launch<kPow, 4, TQ, kSrc>(st, t);
+  }
+  if (TQ > 1 && t.P.lines >= 2 * 16 * 256) return launch<kPow, 2, TQ, kSrc>(st, t);
+  return launch<kPow, 1, TQ, kSrc>(st, t);
+}
+
+template <bool kPow>
+hipError_t launch_tokens(hipStream_t st, const F8Token& t) {
   if (t.x) {
     switch (t.src) {
-      case OZFP4_F32: return launch<kExact, kMode, FP, FQ, 1, OZFP4_F32>(st, t);
-      case OZFP4_BF16: return launch<kExact, kMode, FP, FQ, 1, OZFP4_BF16>(st, t);
-      default: return launch<kExact, kMode, FP, FQ, 1, OZFP4_F16>(st, t);
+      case OZFP4_F32: return launch_lines<kPow, 1, OZFP4_F32>(st, t);
+      case OZFP4_BF16: return launch_lines<kPow, 1, OZFP4_BF16>(st, t);
+      default: return launch_lines<kPow, 1, OZFP4_F16>(st, t);
     }
   }
-  if (t.Q.lines <= 16) return launch<kExact, kMode, FP, FQ, 1, -1>(st, t);
-  if (t.Q.lines <= 32) return launch<kExact, kMode, FP, FQ, 2, -1>(st, t);
-  return launch<kExact, kMode, FP, FQ, 4, -1>(st, t);
-}
-
-template <bool kExact, int FP, int FQ>
-hipError_t launch_mode(hipStream_t st, const F8Token& t) {
-  if (t.pow2) return launch_lines<kExact, kPow2, FP, FQ>(st, t);
-  if (t.P.shift) return launch_lines<kExact, kTileP, FP, FQ>(st, t);
-  return launch_lines<kExact, kLineP, FP, FQ>(st, t);
-}
-
-template <int FP, int FQ>
-hipError_t launch_formats(hipStream_t st, const F8Token& t) {
-  return t.type == OZFP4_F32 ? launch_mode<true, FP, FQ>(st, t) : launch_mode<false, FP, FQ>(st, t);
+  if (t.Q.lines <= 16) return launch_lines<kPow, 1, -1>(st, t);
+  if (t.Q.lines <= 32) return launch_lines<kPow, 2, -1>(st, t);
+  return launch_lines<kPow, 4, -1>(st, t);
 }
 
 }  // namespace
 
 hipError_t launch_f8_token(hipStream_t st, const F8Token& t) {
-  switch (t.P.fmt * 2 + t.Q.fmt) {
-    case 0: return launch_formats<0, 0>(st, t);
-    case 1: return launch_formats<0, 1>(st, t);
-    case 2: return launch_formats<1, 0>(st, t);
-    default: return launch_formats<1, 1>(st, t);
-  }
+  return t.pow2 ? launch_tokens<true>(st, t) : launch_tokens<false>(st, t);
 }
 
 }  // namespace ozfp4
