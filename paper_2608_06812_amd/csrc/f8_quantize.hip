@@ -8,22 +8,50 @@
 //   even. |x / S| <= t (1 + 2^-24), which rounds to t, so nothing saturates.
 //   NaN stays NaN; an infinity is NaN in e4m3, which has none, and itself in
 //   e5m2.
-// One block of 256 threads takes 128 x 128 elements of X, held in registers
-// from one read of X, whichever of the two directions are wanted. Memory
-// bound: the bytes are X once and each output once.
+// Two kernels, both bound by memory (X once, each output once): a streaming one
+// where each row has scales of its own and nothing goes the other way, and one
+// that holds 128 x 128 elements of X in registers for the rest, so that both
+// directions come from one read of X.
+#include <algorithm>
+#include <type_traits>
+
+#include "device_common.hpp"
 #include "f8_round.hpp"
 
 namespace ozfp4 {
 namespace {
 
-constexpr int kTLd = 128 + 8;   // bytes from column to column of the transposed tile in LDS
+// A scale per row and 128 columns: sixteen lanes a block of 128, eight
+// columns a lane, four blocks side by side a wave. row0: first row of the launch.
+template <int kSrc, bool kPow2, int kFmt>
+__global__ __launch_bounds__(256) void k_f8_quantize_rows(F8Quantize p, int64_t row0, unsigned chunks) {
+  typedef typename Source<kSrc>::T T;
+  const int t = threadIdx.x, cg = t & 15;
+  const unsigned chunk = blockIdx.x % chunks;          // 16 blocks of 128 columns
+  const int64_t row = row0 + blockIdx.x / chunks;
+  const int64_t b = (int64_t)chunk * 16 + (t >> 4), col = b * 128 + cg * 8;
+  if (b * 128 >= p.cols) return;                       // whole sixteens of lanes
+  float x[8];
+  load8(static_cast<const T*>(p.x) + row * p.ldx + col, p.cols - col, x);
+  float a = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) a = __builtin_fmaxf(a, finite_abs(x[j]));
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
+  const uint2 w = pack8<kPow2, true, kFmt>(x, make_scale<kPow2, kFmt>(a));
+  if (col < p.cols)   // the line's padding to 16 takes what is behind cols
+    *reinterpret_cast<uint2*>(p.q1 + row * p.ld1 + col) = w;
+  if (cg == 0) store_scale<kPow2, kFmt>(p.s1, row * p.s1l + b * p.s1k, a);
+}
 
 // Thread t holds columns 8 (t % 16) .. + 7 of rows 8 (t / 16) .. + 7: a row's
-// 128 columns are 16 neighbouring lanes, a wave has 32 rows.
+// 128 columns are 16 neighbouring lanes, a wave has 32 rows. The turned values
+// pass through LDS, where column c has 16 units of 8 rows, unit u at u ^ (c /
+// 8): a wave's writes then fall on all banks alike.
 template <int kSrc, bool kPow2, int kFmt>
 __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tiles_c) {
   typedef typename Source<kSrc>::T T;
-  __shared__ __align__(16) uint8_t turned[128 * kTLd];
+  __shared__ __align__(16) uint8_t turned[128 * 128];
   __shared__ float colmax[4][128];
   __shared__ float tilemax[4];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -33,36 +61,34 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
 
   float x[8][8];
   const T* src = static_cast<const T*>(p.x) + row0 * p.ldx + col0;
-  const bool whole = col0 + 8 <= p.cols;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool in = row0 + i < p.rows;
-    if (in && whole) {
-      T v[8];
-      __builtin_memcpy(v, src + i * p.ldx, sizeof(v));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[i][j] = widen(v[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[i][j] = in && col0 + j < p.cols ? widen(src[i * p.ldx + j]) : 0.0f;
-    }
-  }
+  for (int i = 0; i < 8; ++i) load8(src + i * p.ldx, row0 + i < p.rows ? p.cols - col0 : 0, x[i]);
 
-  float rowmax[8], cmax[8];
+  // infinities are rare: only a wave that holds one looks at every element
+  float rowmax[8], cmax[8], most = 0.0f;
+  auto largest = [&](auto abs_of) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rowmax[i] = cmax[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) rowmax[i] = cmax[i] = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = finite_abs(x[i][j]);
-      rowmax[i] = __builtin_fmaxf(rowmax[i], a);
-      cmax[j] = __builtin_fmaxf(cmax[j], a);
-    }
+      for (int j = 0; j < 8; ++j) {
+        rowmax[i] = __builtin_fmaxf(rowmax[i], abs_of(x[i][j]));
+        cmax[j] = __builtin_fmaxf(cmax[j], abs_of(x[i][j]));
+      }
+  };
+  largest([](float v) { return __builtin_fabsf(v); });
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = __builtin_fmaxf(most, rowmax[i]);
+  const bool inf = __any(most == __builtin_inff());
+  if (inf) {
+    largest([](float v) { return finite_abs(v); });
+    most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = __builtin_fmaxf(most, rowmax[i]);
+  }
   if (p.tile) {
-    float a = rowmax[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) a = __builtin_fmaxf(a, rowmax[i]);
+    float a = most;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
     if (lane == 0) tilemax[wave] = a;
@@ -111,62 +137,77 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
     }
   }
 
-  if (p.q1) {
+  auto values = [&](auto with_inf) {
+    constexpr bool kInf = decltype(with_inf)::value;
+    if (p.q1) {
+      Scale s = make_scale<kPow2, kFmt>(rowmax[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const Scale s = make_scale<kPow2, kFmt>(rowmax[i]);
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = quotient<kPow2>(x[i][j], s);
-      const uint2 w = {pack4<kFmt>(v[0], v[1], v[2], v[3]), pack4<kFmt>(v[4], v[5], v[6], v[7])};
-      if (row0 + i < p.rows && col0 < p.cols)   // the line's padding to 16 takes what is behind cols
-        *reinterpret_cast<uint2*>(p.q1 + (row0 + i) * p.ld1 + col0) = w;
+      for (int i = 0; i < 8; ++i) {
+        if (i > 0 && !p.tile) s = make_scale<kPow2, kFmt>(rowmax[i]);
+        const uint2 w = pack8<kPow2, kInf, kFmt>(x[i], s);
+        if (row0 + i < p.rows && col0 < p.cols)   // the line's padding to 16 takes what is behind cols
+          *reinterpret_cast<uint2*>(p.q1 + (row0 + i) * p.ld1 + col0) = w;
+      }
     }
-  }
+    if (p.q0) {
+      Scale s = make_scale<kPow2, kFmt>(cmax[0]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j > 0 && !p.tile) s = make_scale<kPow2, kFmt>(cmax[j]);
+        const float v[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
+        *reinterpret_cast<uint2*>(turned + (cg * 8 + j) * 128 + (rg ^ cg) * 8) = pack8<kPow2, kInf, kFmt>(v, s);
+      }
+    }
+  };
+  if (inf)
+    values(std::true_type{});
+  else
+    values(std::false_type{});
   if (p.q0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const Scale s = make_scale<kPow2, kFmt>(cmax[j]);
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = quotient<kPow2>(x[i][j], s);
-      const uint2 w = {pack4<kFmt>(v[0], v[1], v[2], v[3]), pack4<kFmt>(v[4], v[5], v[6], v[7])};
-      *reinterpret_cast<uint2*>(turned + (cg * 8 + j) * kTLd + rg * 8) = w;
-    }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const int c = n * 32 + (t >> 3), piece = (t & 7) * 16;
-      const int64_t col = (int64_t)tc * 128 + c, row = (int64_t)tr * 128 + piece;
+      const int c = n * 32 + (t >> 3), piece = t & 7;   // rows 16 piece .. + 15 of column c
+      const int64_t col = (int64_t)tc * 128 + c, row = (int64_t)tr * 128 + piece * 16;
       if (col < p.cols && row < p.rows) {
-        const uint2 a = *reinterpret_cast<const uint2*>(turned + c * kTLd + piece);
-        const uint2 b = *reinterpret_cast<const uint2*>(turned + c * kTLd + piece + 8);
-        *reinterpret_cast<uint4*>(p.q0 + col * p.ld0 + row) = uint4{a.x, a.y, b.x, b.y};
+        const int f = c >> 3;   // units 2 piece and 2 piece + 1 lie side by side, swapped for odd f
+        const uint4 u = *reinterpret_cast<const uint4*>(turned + c * 128 + ((2 * piece ^ f) & ~1) * 8);
+        *reinterpret_cast<uint4*>(p.q0 + col * p.ld0 + row) = f & 1 ? uint4{u.z, u.w, u.x, u.y} : u;
       }
     }
   }
 }
 
-template <int kSrc, bool kPow2>
-hipError_t launch(hipStream_t st, const F8Quantize& q, int64_t tr, int64_t tc) {
-  const dim3 grid((unsigned)(tr * tc));
-  if (q.fmt == OZFP4_E4M3)
-    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, OZFP4_E4M3>), grid, dim3(256), 0, st, q, (unsigned)tc);
-  else
-    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, OZFP4_E5M2>), grid, dim3(256), 0, st, q, (unsigned)tc);
+template <int kSrc, bool kPow2, int kFmt>
+hipError_t launch_format(hipStream_t st, const F8Quantize& q) {
+  const int64_t tr = (q.rows + 127) / 128, tc = (q.cols + 127) / 128;
+  if (q.q0 || q.tile) {
+    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt>), dim3((unsigned)(tr * tc)), dim3(256), 0, st, q,
+                       (unsigned)tc);
+    return hipGetLastError();
+  }
+  const int64_t chunks = (tc + 15) / 16, most = std::max<int64_t>(1, (kLaunchThreads / 256) / chunks);
+  for (int64_t row = 0; row < q.rows; row += most)
+    hipLaunchKernelGGL((k_f8_quantize_rows<kSrc, kPow2, kFmt>),
+                       dim3((unsigned)(chunks * std::min(most, q.rows - row))), dim3(256), 0, st, q, row,
+                       (unsigned)chunks);
   return hipGetLastError();
+}
+
+template <int kSrc, bool kPow2>
+hipError_t launch(hipStream_t st, const F8Quantize& q) {
+  return q.fmt == OZFP4_E4M3 ? launch_format<kSrc, kPow2, OZFP4_E4M3>(st, q)
+                             : launch_format<kSrc, kPow2, OZFP4_E5M2>(st, q);
 }
 
 }  // namespace
 
 hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize& q) {
-  const int64_t tr = (q.rows + 127) / 128, tc = (q.cols + 127) / 128;
-  if (tr * tc == 0) return hipSuccess;
+  if (q.rows == 0 || q.cols == 0) return hipSuccess;
   switch (q.src) {
-    case OZFP4_F32: return q.pow2 ? launch<OZFP4_F32, true>(st, q, tr, tc) : launch<OZFP4_F32, false>(st, q, tr, tc);
-    case OZFP4_BF16:
-      return q.pow2 ? launch<OZFP4_BF16, true>(st, q, tr, tc) : launch<OZFP4_BF16, false>(st, q, tr, tc);
-    default: return q.pow2 ? launch<OZFP4_F16, true>(st, q, tr, tc) : launch<OZFP4_F16, false>(st, q, tr, tc);
+    case OZFP4_F32: return q.pow2 ? launch<OZFP4_F32, true>(st, q) : launch<OZFP4_F32, false>(st, q);
+    case OZFP4_BF16: return q.pow2 ? launch<OZFP4_BF16, true>(st, q) : launch<OZFP4_BF16, false>(st, q);
+    default: return q.pow2 ? launch<OZFP4_F16, true>(st, q) : launch<OZFP4_F16, false>(st, q);
   }
 }
 

@@ -22,6 +22,9 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < __builtin_inff() ? a : 0.0f;
 }
 
+// max(m, |x|); drops NaN but not infinities
+__device__ __forceinline__ float max_abs(float m, float x) { return __builtin_fmaxf(m, __builtin_fabsf(x)); }
+
 // A block's scale and what its elements need: S = m 2^e, m in [1, 2), and
 // r = fl(1 / m).
 struct Scale {
@@ -71,23 +74,23 @@ __device__ __forceinline__ void store_scale(void* s, int64_t at, float a) {
 // x / S as an FP32 value that rounds to the format as the exact quotient
 // does. The FP32 quotient alone does not: a border between two 8-bit values
 // is itself an FP32 value, and quotients within 2^-25 of it fall on it. So
-// the quotient is rounded to odd: h is within an ulp, the exact residual x -
-// h S says on which side, and an even h (borders are even) that is not exact
-// moves one unit towards the quotient. Dividing x and S by 2^e first keeps the
-// residuals away from underflow for every x that does not round to zero.
-template <bool kPow2>
+// the quotient is rounded to odd: h is within an ulp of it, and the exact
+// residual |x| - h S says whether it is above (then h is the quotient rounded
+// down, else its lower neighbour is) and whether it is h (else the last bit
+// is set, which no border has). Dividing x and S by 2^e first keeps the
+// residuals away from underflow for every x that does not round to zero. NaN
+// stays NaN; an infinity becomes NaN, unless kInf.
+template <bool kPow2, bool kInf>
 __device__ __forceinline__ float quotient(float x, const Scale& s) {
   const float y = __builtin_ldexpf(x, -s.e);
   if constexpr (kPow2) return y;
-  const float q = y * s.r;
-  const float h = __builtin_fmaf(__builtin_fmaf(-q, s.m, y), s.r, q);
-  const float d = __builtin_fmaf(-h, s.m, y);
-  const uint32_t b = __float_as_uint(h);
-  const int step = 1 | ((int)(b ^ __float_as_uint(d)) >> 31);   // +1 away from zero
-  const bool move = d != 0.0f && !(b & 1);
-  const float v = __uint_as_float(move ? b + (uint32_t)step : b);
-  // NaN and infinities as they are; the residuals lose the sign of a zero
-  return __builtin_fabsf(x) < __builtin_inff() ? __builtin_copysignf(v, x) : x;
+  const float a = __builtin_fabsf(y), q = a * s.r;
+  const float h = __builtin_fmaf(__builtin_fmaf(-q, s.m, a), s.r, q);
+  const uint32_t d = __float_as_uint(__builtin_fmaf(-h, s.m, a));
+  const uint32_t b = (__float_as_uint(h) - (d >> 31)) | min(d, 1u);
+  const float v = __builtin_copysignf(__uint_as_float(b), y);
+  if constexpr (kInf) return __builtin_fabsf(x) < __builtin_inff() ? v : x;
+  return v;
 }
 
 template <int kFmt>
@@ -101,6 +104,29 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     v = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, v, true);
   }
   return (uint32_t)v;
+}
+
+// Eight quotients as 8-bit values.
+template <bool kPow2, bool kInf, int kFmt>
+__device__ __forceinline__ uint2 pack8(const float (&x)[8], const Scale& s) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = quotient<kPow2, kInf>(x[j], s);
+  return uint2{pack4<kFmt>(v[0], v[1], v[2], v[3]), pack4<kFmt>(v[4], v[5], v[6], v[7])};
+}
+
+// Eight neighbouring elements from src on, of which n exist (any alignment).
+template <typename T>
+__device__ __forceinline__ void load8(const T* src, int64_t n, float (&x)[8]) {
+  if (n >= 8) {
+    T v[8];
+    __builtin_memcpy(v, src, sizeof(v));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = widen(v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < n ? widen(src[j]) : 0.0f;
+  }
 }
 
 }  // namespace ozfp4

@@ -74,24 +74,14 @@ __device__ __forceinline__ void quantize_tokens(const F8Token& t, int m, int tot
     const int64_t col = (int64_t)b * kF8Block + r * 8;
     const T* src = static_cast<const T*>(t.x) + i * t.ldx + col;
     float x[8], a = 0.0f;
-    if (col + 8 <= t.k) {
-      T v[8];
-      __builtin_memcpy(v, src, sizeof(v));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = widen(v[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = col + e < t.k ? widen(src[e]) : 0.0f;
-    }
+    load8(src, t.k - col, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) a = __builtin_fmaxf(a, finite_abs(x[e]));
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
     const Scale s = make_scale<kPow, kFmt>(a);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = quotient<kPow>(x[e], s);
     *reinterpret_cast<uint2*>(lds + u * 128 + (((r >> 1) ^ (i & 7)) * 16) + (r & 1) * 8) =
-        uint2{pack4<kFmt>(x[0], x[1], x[2], x[3]), pack4<kFmt>(x[4], x[5], x[6], x[7])};
+        pack8<kPow, true, kFmt>(x, s);
     if (r == 0) {
       if constexpr (kPow)
         scales[u] = (uint32_t)(scale_exp<kFmt>(a) + 127);
