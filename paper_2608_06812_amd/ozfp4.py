@@ -577,13 +577,19 @@ def sgemm(A, B, n_moduli: int | None = None, out=None):
 # ----------------------- 8-bit products with a scale for each block of 128
 
 _f8_tables = None
+_raw_stream = _raw_device = None
 
 
 def _f8_types():
     """Codes of (input and output types, 8-bit formats, scale types)."""
-    global _f8_tables
+    global _f8_tables, _raw_stream, _raw_device
     if _f8_tables is None:
         t = _th()
+        # the current stream's handle without a Stream object (1 us of a small
+        # call's 8), where torch has it
+        _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda dev: t.cuda.current_stream(dev).cuda_stream)
+        _raw_device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
         _f8_tables = ({t.float32: OZFP4_F32, t.bfloat16: OZFP4_BF16, t.float16: OZFP4_F16},
                       {t.float8_e4m3fn: OZFP4_E4M3, t.float8_e5m2: OZFP4_E5M2},
                       {t.float32: OZFP4_SCALE_F32, t.float8_e8m0fnu: OZFP4_SCALE_E8M0})
@@ -634,40 +640,41 @@ def _source(X, name):
 
 def _quantized(Q, S, axis, name):
     """F8Matrix of values Q and scales S along `axis`, the scale code, and the
-    tensors that back it."""
+    values that back it."""
     _device_matrix(Q, name)
     _device_matrix(S, "S" + name)
     _, formats, scales = _f8_types()
     fmt = _code(formats, Q.dtype, name)
     kind = _code(scales, S.dtype, "S" + name)
     r, c = Q.shape
-    lines = (_blocks(r), c) if axis == 0 else (r, _blocks(c))
-    tiles = (_blocks(r), _blocks(c))
-    shape = tuple(S.shape)
-    if shape != lines and shape != tiles:
-        raise ValueError(f"S{name} must have shape {lines} or {tiles}, not {shape}")
+    sr, sc = S.shape
+    br, bc = _blocks(r), _blocks(c)
+    if axis == 0:
+        lines = sr == br and sc == c
+    else:
+        lines = sr == r and sc == bc
+    if not lines and not (sr == br and sc == bc):
+        raise ValueError(f"S{name} must have shape {(br, c) if axis == 0 else (r, bc)} or {(br, bc)}, not {(sr, sc)}")
     st = _unit(Q)
     if st is None:
         Q = Q.contiguous()
         st = _unit(Q)
     srs, scs = S.stride()
-    return F8Matrix(Q.data_ptr(), st[0], st[1], S.data_ptr(), srs, scs, fmt, shape != lines), kind, Q
+    return F8Matrix(Q.data_ptr(), st[0], st[1], S.data_ptr(), srs, scs, fmt, 0 if lines else 1), kind, Q
 
 
-def _output(out, shape, dtype, device, name):
+def _output(out, rows, cols, dtype, device, name):
     """`out` or a new row-major tensor, its type code and strides."""
     code = _code(_f8_types()[0], dtype, f"{name}'s type")
     if out is None:
-        C = _th().empty(shape, dtype=dtype, device=device)
-    else:
-        _device_matrix(out, name)
-        C = out
-        if tuple(C.shape) != tuple(shape) or C.dtype != dtype:
-            raise ValueError(f"{name} must be a {str(dtype).split('.')[-1]} tensor of shape {tuple(shape)}")
-    st = _unit(C)
+        return _th().empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device), code, (max(1, cols), 1)
+    _device_matrix(out, name)
+    if tuple(out.shape) != (rows, cols) or out.dtype != dtype:
+        raise ValueError(f"{name} must be a {str(dtype).split('.')[-1]} tensor of shape {(rows, cols)}")
+    st = _unit(out)
     if st is None:
         raise ValueError(f"{name} must be row-major or column-major")
-    return C, code, st
+    return out, code, st
 
 
 def _scratch(nbytes, device):
@@ -680,15 +687,18 @@ def _scratch(nbytes, device):
     return T, T.data_ptr()
 
 
-def _run(device, tensors, call, where):
-    """The library call on `device` and its current stream (see _on)."""
-    torch, dev = _th(), device.index
-    if dev == torch.cuda.current_device() and all(T.get_device() == dev for T in tensors):
-        load().ozfp4_set_stream(torch.cuda.current_stream(dev).cuda_stream)
-        code = call()
+def _run(tensors, fn, args, where):
+    """fn(*args) on the tensors' device and its current stream (see _on)."""
+    dev = tensors[0].get_device()
+    here = dev == _raw_device()
+    for T in tensors:
+        here = here and T.get_device() == dev
+    if here:
+        load().ozfp4_set_stream(_raw_stream(dev))
+        code = fn(*args)
     else:
-        with _on(device, *tensors):
-            code = call()
+        with _on(tensors[0].device, *tensors):
+            code = fn(*args)
     _check(code, where)
 
 
@@ -700,27 +710,30 @@ def _quantize_f8(X, dims, tile, format, scale):
     fmt, kind = _code(formats, format, "format"), _code(scales, scale, "scale")
     X, code, (rs, cs) = _source(X, "X")
     r, c = X.shape
+    device = X.device
     out, mats = [], [None, None]
     S = None
     for dim in dims:
         # lines of adjacent values, 16-byte aligned as the products read them,
         # and scales with the lines adjacent
-        if dim == 1:
-            Q = torch.empty((r, (c + 15) // 16 * 16), dtype=format, device=X.device)[:, :c]
+        lines, k = (r, c) if dim == 1 else (c, r)
+        ld = (k + 15) // 16 * 16 or 16
+        if dim == 1 and ld == k:
+            Q = torch.empty_strided((r, c), (ld, 1), dtype=format, device=device)
         else:
-            Q = torch.empty((c, (r + 15) // 16 * 16), dtype=format, device=X.device)[:, :r].t()
-        if tile:
-            S = torch.empty((_blocks(r), _blocks(c)), dtype=scale, device=X.device) if S is None else S
-        elif dim == 1:
-            S = torch.empty((_blocks(c), r), dtype=scale, device=X.device).t()
-        else:
-            S = torch.empty((_blocks(r), c), dtype=scale, device=X.device)
-        pad = (c if dim == 1 else r) + 15 & ~15
-        strides = (max(16, pad), 1) if dim == 1 else (1, max(16, pad))
-        mats[dim] = F8Matrix(Q.data_ptr(), *strides, S.data_ptr(), *S.stride(), fmt, 1 if tile else 0)
+            Q = torch.empty((lines, ld), dtype=format, device=device)[:, :k]
+            Q = Q if dim == 1 else Q.t()
+        if not tile:
+            S = torch.empty_strided((r, _blocks(c)), (1, max(1, r)), dtype=scale, device=device) if dim == 1 else \
+                torch.empty((_blocks(r), c), dtype=scale, device=device)
+        elif S is None:
+            S = torch.empty((_blocks(r), _blocks(c)), dtype=scale, device=device)
+        srs, scs = S.stride()
+        mats[dim] = F8Matrix(Q.data_ptr(), ld if dim == 1 else 1, 1 if dim == 1 else ld, S.data_ptr(), srs, scs, fmt,
+                             1 if tile else 0)
         out += [Q, S]
     if r > 0 and c > 0:
-        _run(X.device, (X,), lambda: load().ozfp4_quantize_f8(r, c, X.data_ptr(), code, rs, cs, kind, mats[1], mats[0]),
+        _run((X,), load().ozfp4_quantize_f8, (r, c, X.data_ptr(), code, rs, cs, kind, mats[1], mats[0]),
              "ozfp4_quantize_f8")
     return out
 
@@ -766,13 +779,13 @@ def gemm_f8(A, SA, B, SB, out_dtype=None, out=None, accumulate: bool = False):
         raise ValueError("accumulate needs out")
     if out_dtype is None:
         out_dtype = _th().bfloat16 if out is None else out.dtype
-    C, code, (rs, cs) = _output(out, (m, n), out_dtype, A.device, "out")
+    C, code, (rs, cs) = _output(out, m, n, out_dtype, A.device, "out")
     if accumulate and code != OZFP4_F32:
         raise TypeError("accumulate needs a float32 out")
     ws, p = _scratch(ozfp4_gemm_f8_workspace(m, n, k, a, b, rs, cs), A.device)
-    _run(A.device, (A, SA, B, SB, C),
-         lambda: load().ozfp4_gemm_f8(m, n, k, a, b, kind, C.data_ptr(), code, rs, cs, 1 if accumulate else 0, p,
-                                      0 if ws is None else ws.numel()), "ozfp4_gemm_f8")
+    _run((A, SA, B, SB, C), load().ozfp4_gemm_f8,
+         (m, n, k, a, b, kind, C.data_ptr(), code, rs, cs, 1 if accumulate else 0, p, 0 if ws is None else ws.numel()),
+         "ozfp4_gemm_f8")
     return C
 
 
@@ -792,11 +805,11 @@ def linear_f8(X, W, SW, out_dtype=None, format=None, out=None):
         raise ValueError("inner dimensions differ")
     if out_dtype is None:
         out_dtype = X.dtype if out is None else out.dtype
-    Y, code, (rs, cs) = _output(out, (m, n), out_dtype, X.device, "out")
+    Y, code, (rs, cs) = _output(out, m, n, out_dtype, X.device, "out")
     ws, p = _scratch(ozfp4_linear_f8_workspace(m, n, k, w, rs, cs), X.device)
-    _run(X.device, (X, W, SW, Y),
-         lambda: load().ozfp4_linear_f8(m, n, k, X.data_ptr(), x_code, x_rs, x_cs, fmt, w, kind, Y.data_ptr(), code, rs,
-                                        cs, p, 0 if ws is None else ws.numel()), "ozfp4_linear_f8")
+    _run((X, W, SW, Y), load().ozfp4_linear_f8,
+         (m, n, k, X.data_ptr(), x_code, x_rs, x_cs, fmt, w, kind, Y.data_ptr(), code, rs, cs, p,
+          0 if ws is None else ws.numel()), "ozfp4_linear_f8")
     return Y
 
 
@@ -829,15 +842,14 @@ def linear_f8_backward(dY, X, W, SW, format=None, out_dtype=None, dX=None, dW=No
         raise ValueError("accumulate needs dW")
     if out_dtype is None:
         out_dtype = X.dtype if dX is None else dX.dtype
-    dX, code, (dx_rs, dx_cs) = _output(dX, (m, k), out_dtype, X.device, "dX")
-    dW, _, (dw_rs, dw_cs) = _output(dW, (n, k), torch.float32, X.device, "dW")
+    dX, code, (dx_rs, dx_cs) = _output(dX, m, k, out_dtype, X.device, "dX")
+    dW, _, (dw_rs, dw_cs) = _output(dW, n, k, torch.float32, X.device, "dW")
     w.tile = 1
     ws, p = _scratch(ozfp4_linear_f8_backward_workspace(m, n, k, w, dx_rs, dx_cs, dw_rs, dw_cs), X.device)
-    _run(X.device, (dY, X, W, SW, dX, dW),
-         lambda: load().ozfp4_linear_f8_backward(
-             m, n, k, dY.data_ptr(), y_rs, y_cs, fmt, X.data_ptr(), x_rs, x_cs, x_fmt, x_code, w, kind,
-             dX.data_ptr(), code, dx_rs, dx_cs, dW.data_ptr(), dw_rs, dw_cs, 1 if accumulate else 0, p,
-             0 if ws is None else ws.numel()), "ozfp4_linear_f8_backward")
+    _run((dY, X, W, SW, dX, dW), load().ozfp4_linear_f8_backward,
+         (m, n, k, dY.data_ptr(), y_rs, y_cs, fmt, X.data_ptr(), x_rs, x_cs, x_fmt, x_code, w, kind,
+          dX.data_ptr(), code, dx_rs, dx_cs, dW.data_ptr(), dw_rs, dw_cs, 1 if accumulate else 0, p,
+          0 if ws is None else ws.numel()), "ozfp4_linear_f8_backward")
     return dX, dW
 
 
