@@ -43,7 +43,9 @@ struct F8Gemm {
   int vec;           // four adjacent elements of C are aligned for one store
   int stages;        // blocks of 128 a k range holds
   int64_t part;      // elements from one range's C to the next (0: one range)
+  int tile;          // block tile
 };
+enum F8Tile { kF8Tile64, kF8Tile128, kF8Tile256 };   // the last 256 x 128 with an FP32 C
 
 hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g);
 

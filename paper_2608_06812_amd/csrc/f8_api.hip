@@ -2,6 +2,7 @@
 // include/ozfp4.h): argument checks, workspace layout, launches. A workspace
 // query runs the same code as the call, without launching.
 #include <algorithm>
+#include <cstdlib>
 
 #include "f8.hpp"
 #include "ozfp4.h"
@@ -144,6 +145,8 @@ int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, 
   const int64_t size = c.type == OZFP4_F32 ? 4 : 2;
   g.vec = reinterpret_cast<uintptr_t>(c.C) % (4 * size) == 0 && g.ldc % 4 == 0;
   g.stages = (int)std::max<int64_t>(1, blocks_of(k));
+  if (getenv("F8TILE")) g.tile = atoi(getenv("F8TILE")); else
+  g.tile = blocks_of((g.P.lines + 1) / 2) * blocks_of((g.Q.lines + 1) / 2) >= 192 ? kF8Tile256 : kF8Tile64;
   if (!w.fits()) return OZFP4_EWORKSPACE;
   if (w.dry) return OZFP4_OK;
   if (packs) F8_LAUNCH(launch_f8_pack(st, pack, packs));

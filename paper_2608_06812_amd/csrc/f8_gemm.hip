@@ -4,6 +4,8 @@
 // With scales in powers of two the whole sum stays in the matrix cores: an E8M0
 // scale is an operand of the 8-bit instruction, or of the conversion to BF16.
 // An FP32 scale multiplies a block's sum on its way into the FP32 accumulator.
+#include <type_traits>
+
 #include "f8_device.hpp"
 
 namespace ozfp4 {
@@ -40,24 +42,40 @@ __device__ __forceinline__ void store4(const F8Gemm& g, int64_t at, v4f v, int n
       if (e < n) c[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
 }
 
+// LDS DMA of one value of kSize bytes a lane, from base + offset to the word at
+// to + 4 lane (a byte is extended).
+template <int kSize>
+__device__ __forceinline__ void copy_words(const uint8_t* base, uint32_t offset, uint8_t* to) {
+  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, -1, kBufferWord3);
+  auto word = (__attribute__((address_space(3))) void*)to;
+  if constexpr (kSize == 1)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, word, 1, offset, 0, 0, 0);
+  else
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, word, 4, offset, 0, 0, 0);
+}
+
 // Block tile (WP TP 16) lines of P x (WQ TQ 16) of Q, a wave TP x TQ MFMA
 // tiles. A stage is one block of 128 of every line, 128 bytes a line, copied
-// into LDS by buffer-form LDS DMA into kSlots slots, kSlots - 1 stages ahead. A
+// into LDS by buffer-form LDS DMA into kSlots slots. A
 // copy is 8 lines; within a line the 16-byte piece c lies at c ^ (line % 8),
 // which the copy's lanes arrange by the addresses they read, so that the lines
 // of an operand read fall on different banks. The scales of a stage, one word a
-// line, go through registers into LDS beside them.
+// line (a byte is extended on its way), are copied likewise.
 template <bool kExact, int kMode, int FP, int FQ, int WP, int WQ, int TP, int TQ, int kSlots>
-__global__ __launch_bounds__(WP * WQ * 64) void k_f8_gemm(F8Gemm g, unsigned tiles_p, unsigned tiles_q) {
-  constexpr int kThreads = WP * WQ * 64, kWavesN = WP * WQ;
+__global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned tiles_p, unsigned tiles_q) {
+  constexpr int kWavesN = WP * WQ;
   constexpr int BP = WP * TP * 16, BQ = WQ * TQ * 16, kLines = BP + BQ;
   constexpr int kBytes = kLines * kF8Block;
   constexpr int CP = BP / 8 / kWavesN, CQ = BQ / 8 / kWavesN, kCopies = CP + CQ;   // per wave and stage
   static_assert(BP % (8 * kWavesN) == 0 && BQ % (8 * kWavesN) == 0, "whole copies a wave");
-  static_assert(kLines <= kThreads, "a thread a line's scale");
-  static_assert(kSlots == 2 || kSlots == 3, "the wait at a stage's top");
-  __shared__ __align__(1024) uint8_t lds[kSlots * kBytes];
-  __shared__ uint32_t scale[2][kLines];
+  constexpr int kScaleCopies = (kLines / 64 + kWavesN - 1) / kWavesN, kPending = kCopies + kScaleCopies;
+  static_assert(kLines % 64 == 0 && BP % 64 == 0, "a copy of scales belongs to one operand");
+  static_assert(kSlots >= 2 && kSlots <= 4, "the waits for a stage");
+  constexpr int kScaleBytes = kScaleCopies * kWavesN * 256;
+  // one array: with two the compiler tells them apart, and waits for the copies
+  // in flight before every LDS read
+  __shared__ __align__(1024) uint8_t lds[kSlots * (kBytes + kScaleBytes)];
+  uint8_t* const scales = lds + kSlots * kBytes;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -72,7 +90,7 @@ __global__ __launch_bounds__(WP * WQ * 64) void k_f8_gemm(F8Gemm g, unsigned til
 
   // this wave's copies: lines wave * C * 8 + 8 j + lane / 8 of each operand.
   // Lines behind the last are read as the last (their results are not stored),
-  // pieces behind a line's end as its first, and cleared in LDS.
+  // pieces behind a line's end as its first (and left out of the products).
   const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
   auto lines_from = [&](const F8Lines& l, int64_t line) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(l.x + line * l.ld), (short)0, -1, kBufferWord3);
@@ -83,10 +101,27 @@ __global__ __launch_bounds__(WP * WQ * 64) void k_f8_gemm(F8Gemm g, unsigned til
   const uint32_t last_q = (uint32_t)min(g.Q.lines - 1 - q0, (int64_t)BQ - 1) * ldq;
   const uint32_t own_p = (uint32_t)(wave * CP * 8 + (lane >> 3)) * ldp;
   const uint32_t own_q = (uint32_t)(wave * CQ * 8 + (lane >> 3)) * ldq;
+  // and the scales of 64 lines (a wave with none of its own reads the last again)
+  constexpr int kScaleSize = kMode == kPow2 ? 1 : 4;
+  const uint8_t* scale_base[kScaleCopies];
+  int64_t scale_step[kScaleCopies];
+  uint32_t scale_own[kScaleCopies];
+#pragma unroll
+  for (int c = 0; c < kScaleCopies; ++c) {
+    const int line = min((c * kWavesN + wave) * 64, kLines - 64);   // the wave's first, BP on of Q
+    const bool of_p = line < BP;
+    const F8Lines& l = of_p ? g.P : g.Q;
+    const int64_t from = of_p ? p0 + line : q0 + (line - BP), end = l.lines - 1;
+    const int64_t base = min(from, end) >> l.shift;
+    scale_base[c] = static_cast<const uint8_t*>(l.s) + (base * l.sl + first * l.sk) * kScaleSize;
+    scale_step[c] = l.sk * kScaleSize;
+    scale_own[c] = (uint32_t)((min(from + lane, end) >> l.shift) - base) * (uint32_t)(l.sl * kScaleSize);
+  }
+  // stage s into its slot; called for s = 0, 1, 2, ... in turn
   auto copy = [&](int s) {
-    const int st = first + s;
+    const int st = first + s, slot = s % kSlots;
     const uint32_t at = st == total - 1 && (int)piece >= tail ? 0 : piece;
-    uint8_t* to = lds + (s % kSlots) * kBytes;
+    uint8_t* to = lds + slot * kBytes;
 #pragma unroll
     for (int j = 0; j < CP; ++j)
       dma16_buf(from_p, min(own_p + j * 8 * ldp, last_p) + at, (uint32_t)st * kF8Block, to + (wave * CP + j) * 1024);
@@ -94,18 +129,11 @@ __global__ __launch_bounds__(WP * WQ * 64) void k_f8_gemm(F8Gemm g, unsigned til
     for (int j = 0; j < CQ; ++j)
       dma16_buf(from_q, min(own_q + j * 8 * ldq, last_q) + at, (uint32_t)st * kF8Block,
                 to + (BP / 8 + wave * CQ + j) * 1024);
-  };
-
-  // this thread's scale
-  const bool scaling = tid < kLines;
-  const bool sp_of = tid < BP;
-  const F8Lines& sl = sp_of ? g.P : g.Q;
-  const int64_t sline = min(sp_of ? p0 + tid : q0 + (tid - BP), sl.lines - 1) >> sl.shift;
-  auto load_scale = [&](int s) -> uint32_t {
-    if (!scaling || s >= nst) return 0;
-    const int64_t at = sline * sl.sl + (int64_t)(first + s) * sl.sk;
-    if constexpr (kMode == kPow2) return static_cast<const uint8_t*>(sl.s)[at];
-    return static_cast<const uint32_t*>(sl.s)[at];
+#pragma unroll
+    for (int c = 0; c < kScaleCopies; ++c) {
+      copy_words<kScaleSize>(scale_base[c], scale_own[c], scales + slot * kScaleBytes + (c * kWavesN + wave) * 256);
+      scale_base[c] += scale_step[c];
+    }
   };
 
   v4f acc[TP][TQ];
@@ -114,84 +142,159 @@ __global__ __launch_bounds__(WP * WQ * 64) void k_f8_gemm(F8Gemm g, unsigned til
 #pragma unroll
     for (int j = 0; j < TQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
 
-  uint32_t sc = load_scale(0);
-  if (scaling) scale[0][tid] = sc;
-  sc = load_scale(1);
-  if (nst > 0) copy(0);
-  if (kSlots == 3 && nst > 1) copy(1);
-
   // operand reads: line r = lane % 16 of a tile, pieces 2 (lane / 16) and the
   // next one (any order of k will do, as long as both operands have it)
   const int r = lane & 15, h = (lane >> 4) * 2;
   const int o0 = r * 128 + ((h ^ (r & 7)) * 16), o1 = r * 128 + (((h + 1) ^ (r & 7)) * 16);
 
-  for (int s = 0; s < nst; ++s) {
-    // stage s has landed (and the scales of stage s + 1), and every wave has
-    // done with the slot that the next copies go to
-    if (kSlots == 3 && s + 1 < nst)
-      wait_vm_lgkm0<kCopies>();
-    else
-      wait_vm_lgkm0<0>();
-    block_sync();
-    if (scaling) scale[(s + 1) & 1][tid] = sc;
-    if (s + 2 < nst) sc = load_scale(s + 2);
-    if (s + kSlots - 1 < nst) copy(s + kSlots - 1);
-    uint8_t* sb = lds + (s % kSlots) * kBytes;
-    if (first + s == total - 1 && tail < kF8Block) {
-      // zeros behind the end of the lines
-      for (int l = tid; l < kLines; l += kThreads)
-        for (int c = tail / 16; c < 8; ++c) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(sb + l * 128 + ((c ^ (l & 7)) * 16));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int keep = tail - (c * 16 + e * 4);
-            w[e] = keep >= 4 ? w[e] : keep <= 0 ? 0 : w[e] & ((1u << (8 * keep)) - 1);
-          }
-        }
-      wait_vm_lgkm0<0>();
-      block_sync();
-    }
-    const uint32_t* ss = scale[s & 1];
-    const uint8_t* pb = sb + wp * TP * 2048;
-    const uint8_t* qb = sb + (BP + wq * TQ * 16) * 128;
-    auto read = [&](const uint8_t* b) {
-      const v4i x = *reinterpret_cast<const v4i*>(b + o0), y = *reinterpret_cast<const v4i*>(b + o1);
-      return v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    };
-    constexpr uint32_t one = 127;   // E8M0 1
-    Frag<kExact> q[TQ];
-    uint32_t sq[TQ];
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      sq[j] = ss[BP + (wq * TQ + j) * 16 + r];
-      q[j] = Frag<kExact>::template make<FQ>(read(qb + j * 2048), kMode == kPow2 ? sq[j] : one);
-    }
+  // what has been read for the next tile of P and the next stage's Q (in the
+  // 8-bit form straight into the operands), with their scales
+  v8i raw_p, raw_q[kExact ? TQ : 1];
+  Frag<kExact> q[TQ];
+  uint32_t word_p = 0, word_q[TQ];
+  v4f line_p = {1, 1, 1, 1};
+  float tile_p = 1;
+  auto read = [&](const uint8_t* b) {
+    const v4i x = *reinterpret_cast<const v4i*>(b + o0), y = *reinterpret_cast<const v4i*>(b + o1);
+    return v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  };
+  auto words = [&](int s) { return reinterpret_cast<const uint32_t*>(scales + (s % kSlots) * kScaleBytes); };
+  auto read_p = [&](int s, int i) {
+    raw_p = read(lds + (s % kSlots) * kBytes + (wp * TP + i) * 2048);
+    if constexpr (kMode == kPow2) word_p = words(s)[(wp * TP + i) * 16 + r];
+    if constexpr (kMode == kLineP)
+      line_p = *reinterpret_cast<const v4f*>(words(s) + (wp * TP + i) * 16 + (lane >> 4) * 4);
     if constexpr (kMode == kTileP) {
-      const float a = __uint_as_float(ss[wp * TP * 16]);
+      if (i == 0) tile_p = __uint_as_float(words(s)[wp * TP * 16]);
+    }
+  };
+  auto read_q = [&](int s, int j) {
+    const v8i x = read(lds + (s % kSlots) * kBytes + BP * 128 + (wq * TQ + j) * 2048);
+    if constexpr (kExact)
+      raw_q[j] = x;
+    else
+      q[j].x = x;
+    word_q[j] = words(s)[BP + (wq * TQ + j) * 16 + r];
+  };
+
+  // a lane's values behind the end of the lines, in the last stage
+  auto mask = [&](int e) -> uint32_t {
+    const int keep = tail - ((lane >> 4) * 32 + e * 4);
+    return keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1;
+  };
+  auto cut = [&](v8i x) {
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) sq[j] = __float_as_uint(a * __uint_as_float(sq[j]));
+    for (int e = 0; e < 8; ++e) x[e] &= (int)mask(e);
+    return x;
+  };
+
+  // Schedule. A tile of P meets the TQ tiles of Q one by one; with FP32 scales
+  // each product is scaled and added two products later, so that no addition
+  // waits for its product. The next tile of P is read a tile ahead. The handover
+  // to the next stage comes before a stage's last tile of P, whose operands are
+  // in registers by then: its products cover the barrier, the slot is free for
+  // the copies of the stage kSlots on, and each tile of Q is replaced by the
+  // next stage's as soon as its last product is issued.
+  constexpr uint32_t one = 127;   // E8M0 1
+  constexpr int kUnits = TP * TQ;
+  static_assert(kUnits % 4 == 0 && TQ >= 2 && TP % 2 == 0, "products in flight are counted modulo 4");
+  v4f part[4] = {}, line[2] = {};
+  float factor[TQ], before[2] = {0, 0};
+#pragma unroll
+  for (int j = 0; j < TQ; ++j) factor[j] = 0;
+  // product u of a stage (one before its first: of the stage before)
+  auto add = [&](int u) {
+    const int v = (u + kUnits) % kUnits, i = v / TQ, j = v % TQ;
+    const float f = u < 0 ? before[j - (TQ - 2)] : factor[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc[i][j][e] = __builtin_fmaf(kMode == kLineP ? part[v % 4][e] * line[i & 1][e] : part[v % 4][e], f, acc[i][j][e]);
+  };
+
+  // Stage s, with kLeft = min(nst - s, kSlots + 1) stages left: the next one
+  // and the waits are known when the loop is compiled, since branches in a
+  // stage would let the compiler move its products behind the barrier.
+  auto stage = [&](int s, auto left) {
+    constexpr int kLeft = decltype(left)::value;
+    constexpr bool kMore = kLeft > 1;
+    constexpr int kUnderWay = kLeft > kSlots ? kSlots - 2 : kLeft - 2;   // stages copied behind the next one
+    if constexpr (kMode != kPow2) {
+      before[0] = factor[TQ - 2];
+      before[1] = factor[TQ - 1];
+#pragma unroll
+      for (int j = 0; j < TQ; ++j) factor[j] = tile_p * __uint_as_float(word_q[j]);
+    }
+    if constexpr (!kMore) {
+#pragma unroll
+      for (int j = 0; j < TQ; ++j) {
+        if constexpr (kExact)
+          raw_q[j] = cut(raw_q[j]);
+        else
+          q[j].x = cut(q[j].x);
+      }
     }
 #pragma unroll
     for (int i = 0; i < TP; ++i) {
-      uint32_t e8 = one;
-      if constexpr (kMode == kPow2) e8 = ss[(wp * TP + i) * 16 + r];
-      const auto p = Frag<kExact>::template make<FP>(read(pb + i * 2048), e8);
-      v4f sp = {1, 1, 1, 1};
-      if constexpr (kMode == kLineP)
-        sp = *reinterpret_cast<const v4f*>(ss + (wp * TP + i) * 16 + (lane >> 4) * 4);
+      const uint32_t e8 = kMode == kPow2 ? word_p : one;
+      const auto p = Frag<kExact>::template make<FP>(kMore ? raw_p : cut(raw_p), e8);
+      const v4f of_lines = line_p;
+      const bool last = i == TP - 1;
+      if (!last) {
+        read_p(s, i + 1);
+      } else if (kMore) {
+        // the next stage has landed, and every wave has read this one
+        wait_vm_lgkm0<(kMore ? kUnderWay * kPending : 0)>();
+        block_sync();
+        if (kLeft > kSlots) copy(s + kSlots);
+        read_p(s + 1, 0);
+      }
 #pragma unroll
       for (int j = 0; j < TQ; ++j) {
-        if constexpr (kMode == kPow2) {
-          acc[i][j] = block_product<true, FP, FQ>(p, q[j], acc[i][j], e8, sq[j]);
-        } else {
-          const v4f c = block_product<false, FP, FQ>(p, q[j], v4f{0, 0, 0, 0}, 0, 0);
-          const float f = __uint_as_float(sq[j]);
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            acc[i][j][v] = __builtin_fmaf(kMode == kLineP ? c[v] * sp[v] : c[v], f, acc[i][j][v]);
+        if constexpr (kExact) {
+          if (i == 0) q[j] = Frag<kExact>::template make<FQ>(raw_q[j], kMode == kPow2 ? word_q[j] : one);
         }
+        if constexpr (kMode == kPow2) {
+          acc[i][j] = block_product<true, FP, FQ>(p, q[j], acc[i][j], e8, word_q[j]);
+        } else {
+          part[(i * TQ + j) % 4] = block_product<false, FP, FQ>(p, q[j], v4f{0, 0, 0, 0}, 0, 0);
+          add(i * TQ + j - 2);
+          if (j == 1) line[i & 1] = of_lines;
+        }
+        if (last && kMore) read_q(s + 1, j);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+  };
+  if (nst > 0) {
+#pragma unroll
+    for (int a = 0; a < kSlots; ++a)
+      if (a < nst) copy(a);
+    if (kSlots > 3 && nst > 3)
+      wait_vm_lgkm0<(kSlots > 3 ? 3 * kPending : 0)>();
+    else if (kSlots > 2 && nst > 2)
+      wait_vm_lgkm0<(kSlots > 2 ? 2 * kPending : 0)>();
+    else if (nst > 1)
+      wait_vm_lgkm0<kPending>();
+    else
+      wait_vm_lgkm0<0>();
+    block_sync();
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) read_q(0, j);
+    read_p(0, 0);
+    int s = 0;
+    for (; nst - s > kSlots; ++s) stage(s, std::integral_constant<int, kSlots + 1>{});
+    if constexpr (kSlots > 3) {
+      if (nst - s == 4) stage(s++, std::integral_constant<int, 4>{});
+    }
+    if constexpr (kSlots > 2) {
+      if (nst - s == 3) stage(s++, std::integral_constant<int, 3>{});
+    }
+    if (nst - s == 2) stage(s++, std::integral_constant<int, 2>{});
+    stage(s, std::integral_constant<int, 1>{});
+  }
+  if constexpr (kMode != kPow2) {
+    add(kUnits - 2);
+    add(kUnits - 1);
   }
 
 #pragma unroll
@@ -220,12 +323,13 @@ hipError_t launch_tile(hipStream_t st, const F8Gemm& g) {
 
 template <bool kExact, int kMode, int FP, int FQ>
 hipError_t launch_size(hipStream_t st, const F8Gemm& g) {
-  const int64_t big = ((g.P.lines + 255) / 256) * ((g.Q.lines + 255) / 256);
-  if (big >= 192) {
-    if constexpr (kExact) return launch_tile<kExact, kMode, FP, FQ, 4, 2, 4, 4, 3>(st, g);
-    else return launch_tile<kExact, kMode, FP, FQ, 2, 4, 8, 4, 2>(st, g);
+  switch (g.tile) {
+    case kF8Tile256:
+      if constexpr (kExact) return launch_tile<kExact, kMode, FP, FQ, 4, 2, 4, 4, 3>(st, g);
+      else return launch_tile<kExact, kMode, FP, FQ, 2, 4, 8, 4, 2>(st, g);
+    case kF8Tile128: return launch_tile<kExact, kMode, FP, FQ, 2, 2, 4, 4, 4>(st, g);
+    default: return launch_tile<kExact, kMode, FP, FQ, 2, 2, 2, 2, 4>(st, g);
   }
-  return launch_tile<kExact, kMode, FP, FQ, 2, 2, 4, 4, 2>(st, g);
 }
 
 template <bool kExact, int FP, int FQ>
