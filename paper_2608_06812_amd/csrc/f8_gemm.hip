@@ -57,9 +57,12 @@ __device__ __forceinline__ void copy_words(const uint8_t* base, uint32_t offset,
 // Block tile (WP TP 16) lines of P x (WQ TQ 16) of Q, a wave TP x TQ MFMA
 // tiles. A stage is one block of 128 of every line, 128 bytes a line, copied
 // into LDS by buffer-form LDS DMA into kSlots slots. A
-// copy is 8 lines; within a line the 16-byte piece c lies at c ^ (line % 8),
-// which the copy's lanes arrange by the addresses they read, so that the lines
-// of an operand read fall on different banks. The scales of a stage, one word a
+// copy is 8 lines; within a line the 16-byte piece c lies at c ^ (line / 2 % 8),
+// which the copy's lanes arrange by the addresses they read. An operand read
+// takes pieces g and g + 4 of line l % 16 in lane l = 16 g + ..., and the LDS
+// serves lanes 0-3, 12-15 and 20-27 together (then 4-11, 16-19 and 28-31, and
+// the upper half likewise): those fall on all 64 banks. (With pieces 2 g and
+// 2 g + 1 they fall on half of them, and half of the LDS cycles are conflicts.) The scales of a stage, one word a
 // line (a byte is extended on its way), are copied likewise.
 template <bool kExact, int kMode, int FP, int FQ, int WP, int WQ, int TP, int TQ, int kSlots>
 __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned tiles_p, unsigned tiles_q) {
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   constexpr int BP = WP * TP * 16, BQ = WQ * TQ * 16, kLines = BP + BQ;
   constexpr int kBytes = kLines * kF8Block;
   constexpr int CP = BP / 8 / kWavesN, CQ = BQ / 8 / kWavesN, kCopies = CP + CQ;   // per wave and stage
-  static_assert(BP % (8 * kWavesN) == 0 && BQ % (8 * kWavesN) == 0, "whole copies a wave");
+  static_assert(CP % 2 == 0 && CQ % 2 == 0 && BP == 8 * kWavesN * CP && BQ == 8 * kWavesN * CQ, "whole pairs of copies a wave");
   constexpr int kScaleCopies = (kLines / 64 + kWavesN - 1) / kWavesN, kPending = kCopies + kScaleCopies;
   static_assert(kLines % 64 == 0 && BP % 64 == 0, "a copy of scales belongs to one operand");
   static_assert(kSlots >= 2 && kSlots <= 4, "the waits for a stage");
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   // this wave's copies: lines wave * C * 8 + 8 j + lane / 8 of each operand.
   // Lines behind the last are read as the last (their results are not stored),
   // pieces behind a line's end as its first (and left out of the products).
-  const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 4)) * 16;   // of even copies; of odd ones piece ^ 64
   auto lines_from = [&](const F8Lines& l, int64_t line) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(l.x + line * l.ld), (short)0, -1, kBufferWord3);
   };
@@ -120,14 +123,15 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   // stage s into its slot; called for s = 0, 1, 2, ... in turn
   auto copy = [&](int s) {
     const int st = first + s, slot = s % kSlots;
-    const uint32_t at = st == total - 1 && (int)piece >= tail ? 0 : piece;
+    const int end = st == total - 1 ? tail : kF8Block;
+    const uint32_t at[2] = {(int)piece < end ? piece : 0, (int)(piece ^ 64) < end ? piece ^ 64 : 0};
     uint8_t* to = lds + slot * kBytes;
 #pragma unroll
     for (int j = 0; j < CP; ++j)
-      dma16_buf(from_p, min(own_p + j * 8 * ldp, last_p) + at, (uint32_t)st * kF8Block, to + (wave * CP + j) * 1024);
+      dma16_buf(from_p, min(own_p + j * 8 * ldp, last_p) + at[j & 1], (uint32_t)st * kF8Block, to + (wave * CP + j) * 1024);
 #pragma unroll
     for (int j = 0; j < CQ; ++j)
-      dma16_buf(from_q, min(own_q + j * 8 * ldq, last_q) + at, (uint32_t)st * kF8Block,
+      dma16_buf(from_q, min(own_q + j * 8 * ldq, last_q) + at[j & 1], (uint32_t)st * kF8Block,
                 to + (BP / 8 + wave * CQ + j) * 1024);
 #pragma unroll
     for (int c = 0; c < kScaleCopies; ++c) {
@@ -142,10 +146,9 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
 #pragma unroll
     for (int j = 0; j < TQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
 
-  // operand reads: line r = lane % 16 of a tile, pieces 2 (lane / 16) and the
-  // next one (any order of k will do, as long as both operands have it)
-  const int r = lane & 15, h = (lane >> 4) * 2;
-  const int o0 = r * 128 + ((h ^ (r & 7)) * 16), o1 = r * 128 + (((h + 1) ^ (r & 7)) * 16);
+  // operand reads (any order of k will do, as long as both operands have it)
+  const int r = lane & 15, h = lane >> 4;
+  const int o0 = r * 128 + ((h ^ (r >> 1)) * 16), o1 = r * 128 + (((h + 4) ^ (r >> 1)) * 16);
 
   // what has been read for the next tile of P and the next stage's Q (in the
   // 8-bit form straight into the operands), with their scales
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
 
   // a lane's values behind the end of the lines, in the last stage
   auto mask = [&](int e) -> uint32_t {
-    const int keep = tail - ((lane >> 4) * 32 + e * 4);
+    const int keep = tail - (h * 16 + (e >> 2) * 64 + (e & 3) * 4);
     return keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1;
   };
   auto cut = [&](v8i x) {
