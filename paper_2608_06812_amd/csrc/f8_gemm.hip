@@ -120,21 +120,20 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
     scale_step[c] = l.sk * kScaleSize;
     scale_own[c] = (uint32_t)((min(from + lane, end) >> l.shift) - base) * (uint32_t)(l.sl * kScaleSize);
   }
-  // stage s into its slot; called for s = 0, 1, 2, ... in turn
-  auto copy = [&](int s) {
+  // copy n of stage s into its slot; every copy of a stage before the next stage's
+  auto copy = [&](int s, int n) {
     const int st = first + s, slot = s % kSlots;
-    const int end = st == total - 1 ? tail : kF8Block;
-    const uint32_t at[2] = {(int)piece < end ? piece : 0, (int)(piece ^ 64) < end ? piece ^ 64 : 0};
-    uint8_t* to = lds + slot * kBytes;
-#pragma unroll
-    for (int j = 0; j < CP; ++j)
-      dma16_buf(from_p, min(own_p + j * 8 * ldp, last_p) + at[j & 1], (uint32_t)st * kF8Block, to + (wave * CP + j) * 1024);
-#pragma unroll
-    for (int j = 0; j < CQ; ++j)
-      dma16_buf(from_q, min(own_q + j * 8 * ldq, last_q) + at[j & 1], (uint32_t)st * kF8Block,
-                to + (BP / 8 + wave * CQ + j) * 1024);
-#pragma unroll
-    for (int c = 0; c < kScaleCopies; ++c) {
+    if (n < kCopies) {
+      const int end = st == total - 1 ? tail : kF8Block;
+      const uint32_t own = n % 2 ? piece ^ 64 : piece, at = (int)own < end ? own : 0;   // CP is even
+      uint8_t* to = lds + slot * kBytes;
+      if (n < CP)
+        dma16_buf(from_p, min(own_p + n * 8 * ldp, last_p) + at, (uint32_t)st * kF8Block, to + (wave * CP + n) * 1024);
+      else
+        dma16_buf(from_q, min(own_q + (n - CP) * 8 * ldq, last_q) + at, (uint32_t)st * kF8Block,
+                  to + (BP / 8 + wave * CQ + n - CP) * 1024);
+    } else {
+      const int c = n - kCopies;
       copy_words<kScaleSize>(scale_base[c], scale_own[c], scales + slot * kScaleBytes + (c * kWavesN + wave) * 256);
       scale_base[c] += scale_step[c];
     }
@@ -197,9 +196,15 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   // to the next stage comes before a stage's last tile of P, whose operands are
   // in registers by then: its products cover the barrier, the slot is free for
   // the copies of the stage kSlots on, and each tile of Q is replaced by the
-  // next stage's as soon as its last product is issued.
+  // next stage's as soon as its last product is issued. The copies are spread
+  // over the products, one for kEvery of them, from the handover on and into the
+  // next stage: a wave that issues all of them at once waits for the address
+  // unit, which takes 16 cycles a copy, and its products with it.
   constexpr uint32_t one = 127;   // E8M0 1
   constexpr int kUnits = TP * TQ;
+  constexpr int kEvery = kExact || kUnits <= 16 ? 1 : 2;
+  constexpr int kAtOnce = kUnits <= 4 ? kPending : 0, kInLast = kAtOnce ? kAtOnce : TQ / kEvery;
+  static_assert(kInLast + (TP - 1) * TQ / kEvery >= kPending, "a stage's copies end before its handover");
   static_assert(kUnits % 4 == 0 && TQ >= 2 && TP % 2 == 0, "products in flight are counted modulo 4");
   v4f part[4] = {}, line[2] = {};
   float factor[TQ], before[2] = {0, 0};
@@ -248,7 +253,9 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
         // the next stage has landed, and every wave has read this one
         wait_vm_lgkm0<(kMore ? kUnderWay * kPending : 0)>();
         block_sync();
-        if (kLeft > kSlots) copy(s + kSlots);
+        if (kAtOnce && kLeft > kSlots)
+#pragma unroll
+          for (int n = 0; n < kAtOnce; ++n) copy(s + kSlots, n);
         read_p(s + 1, 0);
       }
 #pragma unroll
@@ -264,20 +271,27 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
           if (j == 1) line[i & 1] = of_lines;
         }
         if (last && kMore) read_q(s + 1, j);
+        const int u = i * TQ + j;
+        if (!kAtOnce && last && kLeft > kSlots && j % kEvery == 0) copy(s + kSlots, j / kEvery);
+        if (!last && kLeft >= kSlots && u % kEvery == 0 && kInLast + u / kEvery < kPending)
+          copy(s + kSlots - 1, kInLast + u / kEvery);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
   if (nst > 0) {
+    // the last slot's stage as far as a stage before it would have copied it
 #pragma unroll
     for (int a = 0; a < kSlots; ++a)
-      if (a < nst) copy(a);
+      if (a < nst)
+#pragma unroll
+        for (int n = 0; n < (a < kSlots - 1 ? kPending : kInLast); ++n) copy(a, n);
     if (kSlots > 3 && nst > 3)
-      wait_vm_lgkm0<(kSlots > 3 ? 3 * kPending : 0)>();
+      wait_vm_lgkm0<(kSlots > 3 ? 2 * kPending + kInLast : 0)>();
     else if (kSlots > 2 && nst > 2)
-      wait_vm_lgkm0<(kSlots > 2 ? 2 * kPending : 0)>();
+      wait_vm_lgkm0<(kSlots > 2 ? (kSlots > 3 ? 2 * kPending : kPending + kInLast) : 0)>();
     else if (nst > 1)
-      wait_vm_lgkm0<kPending>();
+      wait_vm_lgkm0<(kSlots > 2 ? kPending : kInLast)>();
     else
       wait_vm_lgkm0<0>();
     block_sync();
