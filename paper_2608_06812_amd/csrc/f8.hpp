@@ -41,13 +41,27 @@ struct F8Gemm {
   int accumulate;    // C is FP32 and added to
   int pow2;          // scales are E8M0 bytes
   int vec;           // four adjacent elements of C are aligned for one store
+  int vec8;          // C is of 16 bits and eight are
   int stages;        // blocks of 128 a k range holds
-  int64_t part;      // elements from one range's C to the next (0: one range)
+  int partial;       // C is FP32, one sum a range,
+  int64_t part;      // elements from one range's C to the next
   int tile;          // block tile
 };
 enum F8Tile { kF8Tile64, kF8Tile128, kF8Tile256 };   // the last 256 x 128 with an FP32 C
 
 hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g);
+
+// C (+)= the sum of `ranges` partial products (q * ldp + p, part elements
+// apart, ldp a multiple of 4), added in their order.
+struct F8Sum {
+  const float* x;
+  int64_t ldp, part, lines_p, lines_q;
+  int ranges;
+  void* C;
+  int64_t ldc;
+  int type, accumulate;
+};
+hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s);
 
 // The same with few lines of Q; element (p, q) at C[p * cp + q * cq]. Lines of
 // any alignment. x (or null): the lines of Q as they are, value kk of line i

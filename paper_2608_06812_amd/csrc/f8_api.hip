@@ -142,15 +142,40 @@ int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, 
   g.type = c.type;
   g.accumulate = c.accumulate;
   g.pow2 = pow2;
-  const int64_t size = c.type == OZFP4_F32 ? 4 : 2;
-  g.vec = reinterpret_cast<uintptr_t>(c.C) % (4 * size) == 0 && g.ldc % 4 == 0;
-  g.stages = (int)std::max<int64_t>(1, blocks_of(k));
-  if (getenv("F8TILE")) g.tile = atoi(getenv("F8TILE")); else
-  g.tile = blocks_of((g.P.lines + 1) / 2) * blocks_of((g.Q.lines + 1) / 2) >= 192 ? kF8Tile256 : kF8Tile64;
+  const int64_t total = blocks_of(k);
+  g.tile = kF8Tile64;
+  int ranges = 1;
+  if (getenv("F8TILE")) { g.tile = atoi(getenv("F8TILE")); ranges = getenv("F8RANGES") ? atoi(getenv("F8RANGES")) : 1; ranges = std::min<int>(ranges, std::max<int>(1, total)); }
+  else g.tile = blocks_of((g.P.lines + 1) / 2) * blocks_of((g.Q.lines + 1) / 2) >= 192 ? kF8Tile256 : kF8Tile64;
+  g.stages = (int)std::max<int64_t>(1, (total + ranges - 1) / ranges);
+  ranges = (int)std::max<int64_t>(1, (total + g.stages - 1) / g.stages);   // none empty
+  F8Sum sum = {};
+  if (ranges > 1) {
+    // FP32 sums of the ranges, then one kernel that adds them in their order
+    sum.ldp = round_up(g.P.lines, 4);
+    sum.part = sum.ldp * g.Q.lines;
+    sum.x = reinterpret_cast<float*>(w.take(sum.part * ranges * 4));
+    sum.lines_p = g.P.lines;
+    sum.lines_q = g.Q.lines;
+    sum.ranges = ranges;
+    sum.C = c.C;
+    sum.ldc = g.ldc;
+    sum.type = c.type;
+    sum.accumulate = c.accumulate;
+    g.part = sum.part;
+    g.C = const_cast<float*>(sum.x);
+    g.ldc = sum.ldp;
+    g.accumulate = 0;
+    g.partial = 1;
+  }
+  const int64_t size = c.type == OZFP4_F32 || g.partial ? 4 : 2;
+  g.vec = reinterpret_cast<uintptr_t>(g.C) % (4 * size) == 0 && g.ldc % 4 == 0;
+  g.vec8 = size == 2 && reinterpret_cast<uintptr_t>(g.C) % 16 == 0 && g.ldc % 8 == 0;
   if (!w.fits()) return OZFP4_EWORKSPACE;
   if (w.dry) return OZFP4_OK;
   if (packs) F8_LAUNCH(launch_f8_pack(st, pack, packs));
   F8_LAUNCH(launch_f8_gemm(st, g));
+  if (ranges > 1) F8_LAUNCH(launch_f8_sum(st, sum));
   return OZFP4_OK;
 }
 

@@ -31,6 +31,7 @@ enum F8Mode { kPow2, kTileP, kLineP };   // E8M0; FP32 with one scale per 128 li
 template <bool kExact> struct Frag;
 
 template <> struct Frag<false> {
+  static constexpr int kSteps = 1;   // instructions a block
   v8i x;
   template <int F>
   static __device__ __forceinline__ Frag make(v8i x, uint32_t) { return {x}; }
@@ -38,6 +39,7 @@ template <> struct Frag<false> {
 
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 template <> struct Frag<true> {
+  static constexpr int kSteps = 4;
   v8b x[4];
   // e8: scale byte
   template <int F>
@@ -63,21 +65,29 @@ template <> struct Frag<true> {
   }
 };
 
-// c + P Q^T over one block; sp, sq: E8M0 bytes (kScaled; the conversion has
-// taken them in the exact form)
+// One of the kSteps instructions of a block's product: c = P Q^T of its part of
+// the block, plus c unless `fresh`. sp, sq: E8M0 bytes (kScaled; the conversion
+// has taken them in the exact form).
 template <bool kScaled, int FP, int FQ>
-__device__ __forceinline__ v4f block_product(const Frag<false>& p, const Frag<false>& q, v4f c, uint32_t sp,
-                                             uint32_t sq) {
+__device__ __forceinline__ void block_step(const Frag<false>& p, const Frag<false>& q, int, v4f& c, bool fresh,
+                                           uint32_t sp, uint32_t sq) {
+  const v4f from = fresh ? v4f{0, 0, 0, 0} : c;
   // constant zero scale operands: the unscaled instruction
   if constexpr (kScaled)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p.x, q.x, c, FP, FQ, 0, (int)sp, 0, (int)sq);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p.x, q.x, from, FP, FQ, 0, (int)sp, 0, (int)sq);
   else
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p.x, q.x, c, FP, FQ, 0, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p.x, q.x, from, FP, FQ, 0, 0, 0, 0);
 }
 template <bool kScaled, int FP, int FQ>
-__device__ __forceinline__ v4f block_product(const Frag<true>& p, const Frag<true>& q, v4f c, uint32_t, uint32_t) {
+__device__ __forceinline__ void block_step(const Frag<true>& p, const Frag<true>& q, int step, v4f& c, bool fresh,
+                                           uint32_t, uint32_t) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p.x[step], q.x[step], fresh ? v4f{0, 0, 0, 0} : c, 0, 0, 0);
+}
+
+// A whole block's product in the exact form.
+__device__ __forceinline__ v4f block_product(const Frag<true>& p, const Frag<true>& q, v4f c) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p.x[i], q.x[i], c, 0, 0, 0);
+  for (int i = 0; i < 4; ++i) block_step<false, 0, 0>(p, q, i, c, false, 0, 0);
   return c;
 }
 

@@ -11,21 +11,9 @@
 namespace ozfp4 {
 namespace {
 
-// Four adjacent elements of C from line p on; n of them exist.
-__device__ __forceinline__ void store4(const F8Gemm& g, int64_t at, v4f v, int n) {
-  if (g.type == OZFP4_F32) {
-    float* c = static_cast<float*>(g.C) + at;
-    if (n >= 4 && g.vec) {
-      v4f* c4 = reinterpret_cast<v4f*>(c);
-      *c4 = g.accumulate ? *c4 + v : v;
-    } else {
-      for (int e = 0; e < 4; ++e)
-        if (e < n) c[e] = g.accumulate ? c[e] + v[e] : v[e];
-    }
-    return;
-  }
-  uint32_t w[2];
-  if (g.type == OZFP4_BF16) {
+// Four values rounded to BF16 or FP16.
+__device__ __forceinline__ void narrow4(int type, v4f v, uint32_t (&w)[2]) {
+  if (type == OZFP4_BF16) {
     typedef __bf16 h4 __attribute__((ext_vector_type(4)));
     const h4 h = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
     __builtin_memcpy(w, &h, 8);
@@ -34,12 +22,43 @@ __device__ __forceinline__ void store4(const F8Gemm& g, int64_t at, v4f v, int n
     const h4 h = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
     __builtin_memcpy(w, &h, 8);
   }
-  uint16_t* c = static_cast<uint16_t*>(g.C) + at;
-  if (n >= 4 && g.vec)
+}
+
+// Four adjacent elements, of which n exist, to C at `at`; vec: aligned for one
+// store.
+__device__ __forceinline__ void store4(void* C, int type, bool add, bool vec, int64_t at, v4f v, int n) {
+  if (type == OZFP4_F32) {
+    float* c = static_cast<float*>(C) + at;
+    if (n >= 4 && vec) {
+      v4f* c4 = reinterpret_cast<v4f*>(c);
+      *c4 = add ? *c4 + v : v;
+    } else {
+      for (int e = 0; e < 4; ++e)
+        if (e < n) c[e] = add ? c[e] + v[e] : v[e];
+    }
+    return;
+  }
+  uint32_t w[2];
+  narrow4(type, v, w);
+  uint16_t* c = static_cast<uint16_t*>(C) + at;
+  if (n >= 4 && vec)
     *reinterpret_cast<uint2*>(c) = uint2{w[0], w[1]};
   else
     for (int e = 0; e < 4; ++e)
       if (e < n) c[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+}
+
+// Memory bound: the partial sums once in, C once out.
+__global__ __launch_bounds__(256) void k_f8_sum(F8Sum s, bool vec) {
+  const int64_t fours = s.ldp / 4, count = fours * s.lines_q;
+  for (int64_t u = blockIdx.x * 256ll + threadIdx.x; u < count; u += gridDim.x * 256ll) {
+    const int64_t q = u / fours, p = (u - q * fours) * 4;
+    const float* x = s.x + q * s.ldp + p;
+    v4f v = *reinterpret_cast<const v4f*>(x);
+    for (int r = 1; r < s.ranges; ++r) v += *reinterpret_cast<const v4f*>(x + r * s.part);
+    const int64_t n = s.lines_p - p;
+    store4(s.C, s.type, s.accumulate, vec, q * s.ldc + p, v, n < 4 ? (int)n : 4);
+  }
 }
 
 // LDS DMA of one value of kSize bytes a lane, from base + offset to the word at
@@ -202,6 +221,7 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   // unit, which takes 16 cycles a copy, and its products with it.
   constexpr uint32_t one = 127;   // E8M0 1
   constexpr int kUnits = TP * TQ;
+  constexpr int kPair = kExact ? 2 : 1;   // products whose instructions alternate
   constexpr int kEvery = kExact || kUnits <= 16 ? 1 : 2;
   constexpr int kAtOnce = kUnits <= 4 ? kPending : 0, kInLast = kAtOnce ? kAtOnce : TQ / kEvery;
   static_assert(kInLast + (TP - 1) * TQ / kEvery >= kPending, "a stage's copies end before its handover");
@@ -259,22 +279,29 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
         read_p(s + 1, 0);
       }
 #pragma unroll
-      for (int j = 0; j < TQ; ++j) {
+      for (int j0 = 0; j0 < TQ; j0 += kPair) {
         if constexpr (kExact) {
-          if (i == 0) q[j] = Frag<kExact>::template make<FQ>(raw_q[j], kMode == kPow2 ? word_q[j] : one);
+#pragma unroll
+          for (int j = j0; j < j0 + kPair; ++j)
+            if (i == 0) q[j] = Frag<kExact>::template make<FQ>(raw_q[j], kMode == kPow2 ? word_q[j] : one);
         }
-        if constexpr (kMode == kPow2) {
-          acc[i][j] = block_product<true, FP, FQ>(p, q[j], acc[i][j], e8, word_q[j]);
-        } else {
-          part[(i * TQ + j) % 4] = block_product<false, FP, FQ>(p, q[j], v4f{0, 0, 0, 0}, 0, 0);
-          add(i * TQ + j - 2);
+#pragma unroll
+        for (int step = 0; step < Frag<kExact>::kSteps; ++step)
+#pragma unroll
+          for (int j = j0; j < j0 + kPair; ++j) {
+            v4f& c = kMode == kPow2 ? acc[i][j] : part[(i * TQ + j) % 4];
+            block_step<kMode == kPow2, FP, FQ>(p, q[j], step, c, kMode != kPow2 && step == 0, e8, word_q[j]);
+          }
+#pragma unroll
+        for (int j = j0; j < j0 + kPair; ++j) {
+          const int u = i * TQ + j;
+          if constexpr (kMode != kPow2) add(u - 2);
           if (j == 1) line[i & 1] = of_lines;
+          if (last && kMore) read_q(s + 1, j);
+          if (!kAtOnce && last && kLeft > kSlots && j % kEvery == 0) copy(s + kSlots, j / kEvery);
+          if (!last && kLeft >= kSlots && u % kEvery == 0 && kInLast + u / kEvery < kPending)
+            copy(s + kSlots - 1, kInLast + u / kEvery);
         }
-        if (last && kMore) read_q(s + 1, j);
-        const int u = i * TQ + j;
-        if (!kAtOnce && last && kLeft > kSlots && j % kEvery == 0) copy(s + kSlots, j / kEvery);
-        if (!last && kLeft >= kSlots && u % kEvery == 0 && kInLast + u / kEvery < kPending)
-          copy(s + kSlots - 1, kInLast + u / kEvery);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -314,15 +341,39 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
     add(kUnits - 1);
   }
 
+  const int64_t pw = p0 + wp * TP * 16, base = (int64_t)range * g.part;
+  if (g.vec8 && !g.partial && pw + TP * 16 <= g.P.lines) {
+    // 16-bit outputs: the words of two tiles change places between the rows of
+    // 16 lanes, so that a lane has eight adjacent lines and four lanes 64 bytes
+    // (with 8 bytes a lane the stores of 4096^2 outputs take 8.5 us, not XX)
+    const int at = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int64_t q = q0 + (wq * TQ + j) * 16 + r;
+#pragma unroll
+      for (int i = 0; i < TP; i += 2) {
+        uint32_t a[2], b[2];
+        narrow4(g.type, acc[i][j], a);
+        narrow4(g.type, acc[i + 1][j], b);
+        const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+        if (q < g.Q.lines)
+          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(g.C) + q * g.ldc + pw + i * 16 + at) =
+              uint4{(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < TQ; ++j) {
     const int64_t q = q0 + (wq * TQ + j) * 16 + r;
     if (q >= g.Q.lines) continue;
 #pragma unroll
     for (int i = 0; i < TP; ++i) {
-      const int64_t p = p0 + (wp * TP + i) * 16 + (lane >> 4) * 4;
-      const int64_t n = g.P.lines - p;
-      if (n > 0) store4(g, (int64_t)range * g.part + q * g.ldc + p, acc[i][j], n < 4 ? (int)n : 4);
+      const int64_t p = pw + i * 16 + (lane >> 4) * 4, n = g.P.lines - p;
+      if (n > 0)
+        store4(g.C, g.partial ? OZFP4_F32 : g.type, g.accumulate, g.vec, base + q * g.ldc + p, acc[i][j],
+               n < 4 ? (int)n : 4);
     }
   }
 }
@@ -370,6 +421,13 @@ hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g) {
     case 2: return launch_formats<1, 0>(st, g);
     default: return launch_formats<1, 1>(st, g);
   }
+}
+
+hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s) {
+  const int64_t size = s.type == OZFP4_F32 ? 4 : 2;
+  const bool vec = reinterpret_cast<uintptr_t>(s.C) % (4 * size) == 0 && s.ldc % 4 == 0;
+  hipLaunchKernelGGL(k_f8_sum, dim3(stride_blocks(s.ldp / 4 * s.lines_q, 256)), dim3(256), 0, st, s, vec);
+  return hipGetLastError();
 }
 
 }  // namespace ozfp4

@@ -199,9 +199,9 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
       auto as_q = [&](int j) { return to_bf16(f.q[j], kPow ? f.sq[j] : one, t.Q.fmt); };
       auto add = [&](int i, int j, const Frag<true>& p, const Frag<true>& q) {
         if constexpr (kPow) {
-          acc[i][j] = block_product<true, 0, 0>(q, p, acc[i][j], 0, 0);
+          acc[i][j] = block_product(q, p, acc[i][j]);
         } else {
-          const v4f c = block_product<false, 0, 0>(q, p, v4f{0, 0, 0, 0}, 0, 0);
+          const v4f c = block_product(q, p, v4f{0, 0, 0, 0});
 #pragma unroll
           for (int v = 0; v < 4; ++v)
             acc[i][j][v] = __builtin_fmaf(c[v], sq[j][v] * __uint_as_float(f.sp[i]), acc[i][j][v]);
