@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "routes.hpp"
+
 namespace ozfp4 {
 
 constexpr int kF8Block = 128;             // contraction values of one scale
@@ -45,9 +47,8 @@ struct F8Gemm {
   int stages;        // blocks of 128 a k range holds
   int partial;       // C is FP32, one sum a range,
   int64_t part;      // elements from one range's C to the next
-  int tile;          // block tile
+  F8Tile tile;
 };
-enum F8Tile { kF8Tile64, kF8Tile128, kF8Tile256 };   // the last 256 x 128 with an FP32 C
 
 hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g);
 
@@ -66,7 +67,7 @@ hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s);
 // The same with few lines of Q; element (p, q) at C[p * cp + q * cq]. Lines of
 // any alignment. x (or null): the lines of Q as they are, value kk of line i
 // at x[i * ldx + kk], quantised in the kernel to Q.fmt.
-constexpr int kF8TokenLines = 64;     // lines of Q, at most; with x 16
+constexpr int kF8TokenLines = 32;     // lines of Q, at most; with x 16
 constexpr int64_t kF8TokenMany = 1 << 26;   // lines of P, at most (one launch)
 constexpr int kF8TokenBlocks = 256;   // with x: lines times blocks of 128, at most
 struct F8Token {

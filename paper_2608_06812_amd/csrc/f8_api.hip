@@ -2,7 +2,6 @@
 // include/ozfp4.h): argument checks, workspace layout, launches. A workspace
 // query runs the same code as the call, without launching.
 #include <algorithm>
-#include <cstdlib>
 
 #include "f8.hpp"
 #include "ozfp4.h"
@@ -142,13 +141,15 @@ int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, 
   g.type = c.type;
   g.accumulate = c.accumulate;
   g.pow2 = pow2;
-  const int64_t total = blocks_of(k);
-  g.tile = kF8Tile64;
-  int ranges = 1;
-  if (getenv("F8TILE")) { g.tile = atoi(getenv("F8TILE")); ranges = getenv("F8RANGES") ? atoi(getenv("F8RANGES")) : 1; ranges = std::min<int>(ranges, std::max<int>(1, total)); }
-  else g.tile = blocks_of((g.P.lines + 1) / 2) * blocks_of((g.Q.lines + 1) / 2) >= 192 ? kF8Tile256 : kF8Tile64;
-  g.stages = (int)std::max<int64_t>(1, (total + ranges - 1) / ranges);
-  ranges = (int)std::max<int64_t>(1, (total + g.stages - 1) / g.stages);   // none empty
+  F8Route route = f8_route(g.P.lines, g.Q.lines, k, c.type == OZFP4_F32);
+  if (w.dry && !c.C) {   // a workspace query: enough for either form
+    const F8Route other = f8_route(g.P.lines, g.Q.lines, k, c.type != OZFP4_F32);
+    if (other.ranges > route.ranges) route = other;
+  }
+  const int64_t total = std::max<int64_t>(1, blocks_of(k));
+  g.tile = route.tile;
+  g.stages = (int)((total + route.ranges - 1) / route.ranges);
+  const int ranges = (int)((total + g.stages - 1) / g.stages);   // none is empty
   F8Sum sum = {};
   if (ranges > 1) {
     // FP32 sums of the ranges, then one kernel that adds them in their order

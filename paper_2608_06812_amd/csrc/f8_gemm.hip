@@ -198,9 +198,10 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
     word_q[j] = words(s)[BP + (wq * TQ + j) * 16 + r];
   };
 
-  // a lane's values behind the end of the lines, in the last stage
+  // a lane's values behind the end of the lines, in the last range's last stage
+  const int end = first + nst == total ? tail : kF8Block;
   auto mask = [&](int e) -> uint32_t {
-    const int keep = tail - (h * 16 + (e >> 2) * 64 + (e & 3) * 4);
+    const int keep = end - (h * 16 + (e >> 2) * 64 + (e & 3) * 4);
     return keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1;
   };
   auto cut = [&](v8i x) {

@@ -15,8 +15,9 @@ struct F8PackPair {
   unsigned tiles[2];  // 128-line tiles of each
 };
 
-// One 128 x 128 tile of bytes through LDS: read along the unit stride, written
-// along k.
+// One 128 x 128 tile of bytes: 16-byte pieces of a line straight from where they
+// lie if k is adjacent, else through LDS, read along the lines and written along
+// k.
 __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
   __shared__ __align__(16) uint8_t tile[kPackTile * kPackLd];
   const int which = blockIdx.x >= two.first;
@@ -24,21 +25,43 @@ __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
   const unsigned b = blockIdx.x - (which ? two.first : 0), nl = two.tiles[which];
   const int64_t l0 = (int64_t)(b % nl) * kPackTile, k0 = (int64_t)(b / nl) * kPackTile;
   const int t = threadIdx.x, sub = t & 31, row = t >> 5;   // 4 bytes of a row of the tile, 8 rows a pass
-  const bool along_k = p.ks == 1;
-  const int64_t a0 = along_k ? l0 : k0, as = along_k ? p.ls : p.ks, an = along_k ? p.lines : p.k;
-  const int64_t u0 = along_k ? k0 : l0, un = along_k ? p.k : p.lines;
+  if (p.ks == 1) {
+    uint4 w[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
+      w[n] = uint4{0, 0, 0, 0};
+      if (line >= p.lines || kk >= p.k) continue;
+      const uint8_t* src = p.x + line * p.ls + kk;
+      if (kk + 16 <= p.k) {
+        __builtin_memcpy(&w[n], src, 16);
+      } else {   // zeros behind the end of the line
+        uint32_t v[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 15; ++e)
+          if (kk + e < p.k) v[e >> 2] |= (uint32_t)src[e] << (8 * (e & 3));
+        w[n] = uint4{v[0], v[1], v[2], v[3]};
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
+      if (line < p.lines && kk < p.k) *reinterpret_cast<uint4*>(p.out + line * p.ld + kk) = w[n];
+    }
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < 16; ++n) {
     const int r = n * 8 + row;
-    const int64_t a = a0 + r, u = u0 + sub * 4;
+    const int64_t a = k0 + r, u = l0 + sub * 4;
     uint32_t w = 0;
-    if (a < an) {
-      const uint8_t* src = p.x + a * as + u;
-      if (u + 4 <= un)
+    if (a < p.k) {
+      const uint8_t* src = p.x + a * p.ks + u;
+      if (u + 4 <= p.lines)
         __builtin_memcpy(&w, src, 4);
       else
         for (int e = 0; e < 4; ++e)
-          if (u + e < un) w |= (uint32_t)src[e] << (8 * e);
+          if (u + e < p.lines) w |= (uint32_t)src[e] << (8 * e);
     }
     *reinterpret_cast<uint32_t*>(tile + r * kPackLd + sub * 4) = w;
   }
@@ -47,14 +70,9 @@ __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
 #pragma unroll
   for (int n = 0; n < 16; ++n) {
     const int l = n * 8 + row;
-    uint32_t w;
-    if (along_k) {
-      w = *reinterpret_cast<const uint32_t*>(tile + l * kPackLd + sub * 4);
-    } else {
-      w = 0;
+    uint32_t w = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w |= (uint32_t)tile[(sub * 4 + e) * kPackLd + l] << (8 * e);
-    }
+    for (int e = 0; e < 4; ++e) w |= (uint32_t)tile[(sub * 4 + e) * kPackLd + l] << (8 * e);
     // the rest of a line's last 16 bytes is written with zeros
     const int64_t line = l0 + l, kk = k0 + sub * 4;
     if (line < p.lines && kk < p.ld && kk < ((p.k + 15) & ~int64_t(15)))

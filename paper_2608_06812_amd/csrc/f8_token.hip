@@ -277,8 +277,8 @@ template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
   if constexpr (TQ == 2) {
     if (t.P.lines >= 4 * 16 * 256) return launch<kPow, 4, TQ, kSrc>(st, t);
+    if (t.P.lines >= 2 * 16 * 256) return launch<kPow, 2, TQ, kSrc>(st, t);
   }
-  if (TQ > 1 && t.P.lines >= 2 * 16 * 256) return launch<kPow, 2, TQ, kSrc>(st, t);
   return launch<kPow, 1, TQ, kSrc>(st, t);
 }
 
@@ -292,8 +292,7 @@ hipError_t launch_tokens(hipStream_t st, const F8Token& t) {
     }
   }
   if (t.Q.lines <= 16) return launch_lines<kPow, 1, -1>(st, t);
-  if (t.Q.lines <= 32) return launch_lines<kPow, 2, -1>(st, t);
-  return launch_lines<kPow, 4, -1>(st, t);
+  return launch_lines<kPow, 2, -1>(st, t);
 }
 
 }  // namespace
