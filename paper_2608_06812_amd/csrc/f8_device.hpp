@@ -26,6 +26,30 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 enum F8Mode { kPow2, kTileP, kLineP };   // E8M0; FP32 with one scale per 128 lines of P; FP32 per line
 
+// The n < 16 last bytes of a line that starts at `line` (n <= 0: none), from p
+// on, and zeros: the 16 bytes that end with the line, moved down, or one by one
+// where the line is shorter than that.
+__device__ __forceinline__ v4i load_end(const uint8_t* line, const uint8_t* p, int n) {
+  uint64_t w[2] = {0, 0};
+  if (n > 0) {
+    if (p + n - line >= 16) {
+      __builtin_memcpy(w, p + n - 16, 16);
+      const int bits = 8 * (16 - n);
+      w[0] = bits >= 64 ? w[1] >> (bits - 64) : w[0] >> bits | w[1] << (64 - bits);
+      w[1] = bits >= 64 ? 0 : w[1] >> bits;
+    } else {
+#pragma unroll 1
+      for (int e = n - 1; e >= 0; --e) {
+        w[1] = w[1] << 8 | w[0] >> 56;
+        w[0] = w[0] << 8 | p[e];
+      }
+    }
+  }
+  v4i v;
+  __builtin_memcpy(&v, w, 16);
+  return v;
+}
+
 // A 16 x 128 operand: line lane % 16, 32 values a lane (v8i), which the
 // instructions take in any order that both operands share.
 template <bool kExact> struct Frag;

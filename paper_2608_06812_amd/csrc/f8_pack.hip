@@ -1,7 +1,7 @@
 // Relayout of 8-bit operands: lines of adjacent values, 16-byte aligned, as
 // the products read them (f8_gemm.hip), from any storage order and alignment.
 // Memory bound: the operand's bytes once in and once out.
-#include "f8.hpp"
+#include "f8_device.hpp"
 
 namespace ozfp4 {
 namespace {
@@ -35,12 +35,9 @@ __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
       const uint8_t* src = p.x + line * p.ls + kk;
       if (kk + 16 <= p.k) {
         __builtin_memcpy(&w[n], src, 16);
-      } else {   // zeros behind the end of the line
-        uint32_t v[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 15; ++e)
-          if (kk + e < p.k) v[e >> 2] |= (uint32_t)src[e] << (8 * (e & 3));
-        w[n] = uint4{v[0], v[1], v[2], v[3]};
+      } else {
+        const v4i v = load_end(src - kk, src, (int)(p.k - kk));
+        __builtin_memcpy(&w[n], &v, 16);
       }
     }
 #pragma unroll

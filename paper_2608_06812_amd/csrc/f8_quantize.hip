@@ -44,58 +44,61 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(F8Quantize p, int64_t 
   if (cg == 0) store_scale<kPow2, kFmt>(p.s1, row * p.s1l + b * p.s1k, a);
 }
 
-// Thread t holds columns 8 (t % 16) .. + 7 of rows 8 (t / 16) .. + 7: a row's
-// 128 columns are 16 neighbouring lanes, a wave has 32 rows. The turned values
-// pass through LDS, where column c has 16 units of 8 rows, unit u at u ^ (c /
-// 8): a wave's writes then fall on all banks alike.
-template <int kSrc, bool kPow2, int kFmt>
-__global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tiles_c) {
+// Thread t holds columns 8 (t % 16) .. + 7 of kRows rows from kRows (t / 16) on:
+// a row's 128 columns are 16 neighbouring lanes. The turned values pass through
+// LDS, where column c has 16 units of 8 rows, unit u at u ^ (c / 8): a wave's
+// writes then fall on all banks alike.
+template <int kSrc, bool kPow2, int kFmt, int kRows>
+__global__ __launch_bounds__(2048 / kRows) void k_f8_quantize(F8Quantize p, unsigned tiles_c) {
   typedef typename Source<kSrc>::T T;
+  constexpr int kThreads = 2048 / kRows, kWavesN = kThreads / 64;
   __shared__ __align__(16) uint8_t turned[128 * 128];
-  __shared__ float colmax[4][128];
-  __shared__ float tilemax[4];
+  __shared__ float colmax[kWavesN][128];
+  __shared__ float tilemax[kWavesN];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int cg = t & 15, rg = t >> 4;
   const unsigned tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-  const int64_t row0 = (int64_t)tr * 128 + rg * 8, col0 = (int64_t)tc * 128 + cg * 8;
+  const int64_t row0 = (int64_t)tr * 128 + rg * kRows, col0 = (int64_t)tc * 128 + cg * 8;
 
-  float x[8][8];
+  float x[kRows][8];
   const T* src = static_cast<const T*>(p.x) + row0 * p.ldx + col0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8(src + i * p.ldx, row0 + i < p.rows ? p.cols - col0 : 0, x[i]);
+  for (int i = 0; i < kRows; ++i) load8(src + i * p.ldx, row0 + i < p.rows ? p.cols - col0 : 0, x[i]);
 
   // infinities are rare: only a wave that holds one looks at every element
-  float rowmax[8], cmax[8], most = 0.0f;
+  float rowmax[kRows], cmax[8], most = 0.0f;
   auto largest = [&](auto abs_of) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rowmax[i] = cmax[i] = 0.0f;
+    for (int j = 0; j < 8; ++j) cmax[j] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kRows; ++i) {
+      rowmax[i] = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         rowmax[i] = __builtin_fmaxf(rowmax[i], abs_of(x[i][j]));
         cmax[j] = __builtin_fmaxf(cmax[j], abs_of(x[i][j]));
       }
-  };
-  largest([](float v) { return __builtin_fabsf(v); });
-#pragma unroll
-  for (int i = 0; i < 8; ++i) most = __builtin_fmaxf(most, rowmax[i]);
-  const bool inf = __any(most == __builtin_inff());
-  if (inf) {
-    largest([](float v) { return finite_abs(v); });
+    }
     most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = __builtin_fmaxf(most, rowmax[i]);
-  }
+    for (int i = 0; i < kRows; ++i) most = __builtin_fmaxf(most, rowmax[i]);
+  };
+  largest([](float v) { return __builtin_fabsf(v); });
+  const bool inf = __any(most == __builtin_inff());
+  if (inf) largest([](float v) { return finite_abs(v); });
   if (p.tile) {
     float a = most;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) a = __builtin_fmaxf(a, __shfl_xor(a, d));
     if (lane == 0) tilemax[wave] = a;
     __syncthreads();
-    a = __builtin_fmaxf(__builtin_fmaxf(tilemax[0], tilemax[1]), __builtin_fmaxf(tilemax[2], tilemax[3]));
+    a = tilemax[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rowmax[i] = cmax[i] = a;
+    for (int w = 1; w < kWavesN; ++w) a = __builtin_fmaxf(a, tilemax[w]);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) rowmax[i] = a;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cmax[j] = a;
     if (t == 0) {
       if (p.q1) store_scale<kPow2, kFmt>(p.s1, tr * p.s1l + tc * p.s1k, a);
       if (p.q0) store_scale<kPow2, kFmt>(p.s0, tc * p.s0l + tr * p.s0k, a);
@@ -103,13 +106,13 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
   } else {
     if (p.q1) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) rowmax[i] = __builtin_fmaxf(rowmax[i], __shfl_xor(rowmax[i], d));
-      if (cg < 8 && row0 + cg < p.rows) {   // lane cg of the row's sixteen stores row cg
+      if (cg < kRows && row0 + cg < p.rows) {   // lane cg of the row's sixteen stores row cg
         float a = rowmax[0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) a = cg == i ? rowmax[i] : a;
+        for (int i = 1; i < kRows; ++i) a = cg == i ? rowmax[i] : a;
         store_scale<kPow2, kFmt>(p.s1, (row0 + cg) * p.s1l + (int64_t)tc * p.s1k, a);
       }
     }
@@ -123,17 +126,17 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
 #pragma unroll
         for (int j = 0; j < 8; ++j) colmax[wave][cg * 8 + j] = cmax[j];
       __syncthreads();
+      if (t < 128) {   // the waves' maxima into the first's
+        float a = colmax[0][t];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = cg * 8 + j;
-        cmax[j] = __builtin_fmaxf(__builtin_fmaxf(colmax[0][c], colmax[1][c]),
-                                  __builtin_fmaxf(colmax[2][c], colmax[3][c]));
+        for (int w = 1; w < kWavesN; ++w) a = __builtin_fmaxf(a, colmax[w][t]);
+        colmax[0][t] = a;
+        if ((int64_t)tc * 128 + t < p.cols)
+          store_scale<kPow2, kFmt>(p.s0, ((int64_t)tc * 128 + t) * p.s0l + (int64_t)tr * p.s0k, a);
       }
-      if (t < 128 && (int64_t)tc * 128 + t < p.cols) {
-        const float a = __builtin_fmaxf(__builtin_fmaxf(colmax[0][t], colmax[1][t]),
-                                        __builtin_fmaxf(colmax[2][t], colmax[3][t]));
-        store_scale<kPow2, kFmt>(p.s0, ((int64_t)tc * 128 + t) * p.s0l + (int64_t)tr * p.s0k, a);
-      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cmax[j] = colmax[0][cg * 8 + j];
     }
   }
 
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
     if (p.q1) {
       Scale s = make_scale<kPow2, kFmt>(rowmax[0]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kRows; ++i) {
         if (i > 0 && !p.tile) s = make_scale<kPow2, kFmt>(rowmax[i]);
         const uint2 w = pack8<kPow2, kInf, kFmt>(x[i], s);
         if (row0 + i < p.rows && col0 < p.cols)   // the line's padding to 16 takes what is behind cols
@@ -154,8 +157,16 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (j > 0 && !p.tile) s = make_scale<kPow2, kFmt>(cmax[j]);
-        const float v[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
-        *reinterpret_cast<uint2*>(turned + (cg * 8 + j) * 128 + (rg ^ cg) * 8) = pack8<kPow2, kInf, kFmt>(v, s);
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) v[i] = x[i][j];
+        const uint2 w = pack8<kPow2, kInf, kFmt>(v, s);
+        const int unit = rg * kRows / 8, within = rg * kRows % 8;
+        uint8_t* to = turned + (cg * 8 + j) * 128 + (unit ^ cg) * 8 + within;
+        if constexpr (kRows == 8)
+          *reinterpret_cast<uint2*>(to) = w;
+        else
+          *reinterpret_cast<uint16_t*>(to) = (uint16_t)w.x;
       }
     }
   };
@@ -166,8 +177,8 @@ __global__ __launch_bounds__(256) void k_f8_quantize(F8Quantize p, unsigned tile
   if (p.q0) {
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int c = n * 32 + (t >> 3), piece = t & 7;   // rows 16 piece .. + 15 of column c
+    for (int n = t; n < 1024; n += kThreads) {
+      const int c = n >> 3, piece = n & 7;   // rows 16 piece .. + 15 of column c
       const int64_t col = (int64_t)tc * 128 + c, row = (int64_t)tr * 128 + piece * 16;
       if (col < p.cols && row < p.rows) {
         const int f = c >> 3;   // units 2 piece and 2 piece + 1 lie side by side, swapped for odd f
@@ -182,8 +193,13 @@ template <int kSrc, bool kPow2, int kFmt>
 hipError_t launch_format(hipStream_t st, const F8Quantize& q) {
   const int64_t tr = (q.rows + 127) / 128, tc = (q.cols + 127) / 128;
   if (q.q0 || q.tile) {
-    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt>), dim3((unsigned)(tr * tc)), dim3(256), 0, st, q,
-                       (unsigned)tc);
+    // few tiles: four times the threads a tile, two rows each
+    if (tr * tc <= 512)
+      hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt, 2>), dim3((unsigned)(tr * tc)), dim3(1024), 0, st, q,
+                         (unsigned)tc);
+    else
+      hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt, 8>), dim3((unsigned)(tr * tc)), dim3(256), 0, st, q,
+                         (unsigned)tc);
     return hipGetLastError();
   }
   const int64_t chunks = (tc + 15) / 16, most = std::max<int64_t>(1, (kLaunchThreads / 256) / chunks);

@@ -23,32 +23,22 @@ namespace {
 
 constexpr int kTokWaves = 8;
 
-// n < 16 bytes, the rest zero
-__device__ __forceinline__ v4i load_some(const uint8_t* p, int n) {
-  uint32_t w[4] = {0, 0, 0, 0};
+// The 32 values of lane group g in the block that starts at byte `at` of a line:
+// 16-byte pieces g and g + 4, of which `left` bytes exist (kWhole: all). Any
+// alignment.
+template <bool kWhole>
+__device__ __forceinline__ v8i load_block(const uint8_t* line, int64_t at, int g, int left) {
+  v4i v[2];
 #pragma unroll
-  for (int e = 0; e < 15; ++e)
-    if (e < n) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
-  return v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
-}
-
-// The 16 bytes of piece c of a line's block, of which `left` bytes exist.
-// Any alignment.
-template <bool kWhole>
-__device__ __forceinline__ v4i load_piece(const uint8_t* block, int c, int left) {
-  const uint8_t* p = block + c * 16;
-  if constexpr (!kWhole) {
-    if (c * 16 + 16 > left) return load_some(p, left - c * 16);
+  for (int h = 0; h < 2; ++h) {
+    const int c = (g + 4 * h) * 16;
+    const uint8_t* p = line + at + c;
+    if (kWhole || c + 16 <= left)
+      __builtin_memcpy(&v[h], p, 16);
+    else
+      v[h] = load_end(line, p, left - c);
   }
-  v4i v;
-  __builtin_memcpy(&v, p, 16);
-  return v;
-}
-
-template <bool kWhole>
-__device__ __forceinline__ v8i load_block(const uint8_t* block, int g, int left) {
-  const v4i x = load_piece<kWhole>(block, g, left), y = load_piece<kWhole>(block, g + 4, left);
-  return v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  return v8i{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 }
 
 template <bool kPow2>
@@ -134,10 +124,10 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
     const int64_t at = (int64_t)s * kF8Block;
     auto blocks = [&](auto whole, int left) {
 #pragma unroll
-      for (int i = 0; i < TP; ++i) f.p[i] = load_block<decltype(whole)::value>(px[i] + at, g, left);
+      for (int i = 0; i < TP; ++i) f.p[i] = load_block<decltype(whole)::value>(px[i], at, g, left);
       if constexpr (!kFused) {
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) f.q[j] = load_block<decltype(whole)::value>(qx[j] + at, g, left);
+        for (int j = 0; j < TQ; ++j) f.q[j] = load_block<decltype(whole)::value>(qx[j], at, g, left);
       }
     };
     if (s == total - 1 && tail < kF8Block)
@@ -276,7 +266,7 @@ hipError_t launch(hipStream_t st, const F8Token& t) {
 template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
   if constexpr (TQ == 2) {
-    if (t.P.lines >= 4 * 16 * 256) return launch<kPow, 4, TQ, kSrc>(st, t);
+    if (kPow && t.P.lines >= 4 * 16 * 256) return launch<kPow, 4, TQ, kSrc>(st, t);   // FP32 scales: no registers
     if (t.P.lines >= 2 * 16 * 256) return launch<kPow, 2, TQ, kSrc>(st, t);
   }
   return launch<kPow, 1, TQ, kSrc>(st, t);

@@ -153,6 +153,23 @@ def test_quantize_extremes(gpu_lib, fmt, scale):
     check_quantize(gpu_lib, h, 2, False, fmt, scale)
 
 
+@pytest.mark.parametrize("fmt", [E4, E5])
+def test_quantize_every_significand(gpu_lib, fmt):
+    """The FP32 scale of every 24-bit significand, in the middle of the range and
+    where the scale becomes the least: the quotient rounded once."""
+    m = torch.arange(1 << 23, dtype=torch.int32, device="cuda")
+    top = float(plain.table(fmt)[-1])
+    for exponent in (127, 10):
+        a = (m | (exponent << 23)).view(torch.float32)
+        x = torch.zeros((1 << 12, 1 << 11, 128), device="cuda")
+        x[:, :, 77] = -a.view(1 << 12, 1 << 11)
+        announce(f"scales of every significand, exponent {exponent}, {fmt}")
+        q, s = gpu_lib.quantize_f8(x.view(1 << 12, 1 << 18), 1, False, fmt, F32)
+        want = (a.double() / torch.full_like(a, top, dtype=torch.float64)).float().clamp(min=2.0 ** -126)
+        assert torch.equal(s, want.view(1 << 12, 1 << 11))
+        del x, q
+
+
 def test_quantize_layouts(gpu_lib):
     """Column-major inputs, views whose rows are not 16-byte aligned, strides
     that have to be copied, and an expanded row."""
