@@ -36,6 +36,7 @@ struct F8Lines {
 // C[p + q * ldc] (+)= sum over k; P's lines are the adjacent ones of C.
 struct F8Gemm {
   F8Lines P, Q;
+  int turned;        // P's lines are adjacent, its k values P.ld bytes apart
   int64_t k;
   void* C;
   int64_t ldc;

@@ -80,6 +80,11 @@ bool in_place(const Operand& o, int64_t k) {
   return o.l.lines == 1 || (o.l.ld % 16 == 0 && o.l.ld <= kF8MaxLd);
 }
 
+// The kernel's P also with its lines adjacent.
+bool in_place_turned(const Operand& o) {
+  return o.l.ld == 1 && o.ks % 16 == 0 && o.ks <= kF8MaxLd && reinterpret_cast<uintptr_t>(o.l.x) % 16 == 0;
+}
+
 // An output matrix of the caller.
 struct Out {
   void* C;
@@ -114,9 +119,17 @@ int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, 
   const bool few_rows = A.l.lines <= B.l.lines;
   const bool tokens = k > 0 && std::min(A.l.lines, B.l.lines) <= kF8TokenLines &&
                       std::max(A.l.lines, B.l.lines) <= kF8TokenMany;
+  // the lines of the operand along which C is adjacent are the kernel's P
+  const bool row_major = c.cs == 1;
+  F8Gemm g = {};
   F8Pack pack[2];
   int packs = 0;
   for (Operand* o : {&A, &B}) {
+    if (!tokens && k > 1 && o == (row_major ? &B : &A) && !in_place(*o, k) && in_place_turned(*o)) {
+      g.turned = 1;
+      o->l.ld = o->ks;
+      continue;
+    }
     if (k == 0 || in_place(*o, k) || (tokens && (o->ks == 1 || k == 1))) continue;
     const int64_t ld = round_up(k, 128);
     pack[packs++] = {o->l.x, o->l.ld, o->ks, o->l.lines, k, w.take(o->l.lines * ld), ld};
@@ -130,9 +143,6 @@ int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, 
     F8_LAUNCH(launch_f8_token(st, token_product(k, few_rows ? A : B, few_rows ? B : A, few_rows, pow2, c)));
     return OZFP4_OK;
   }
-  F8Gemm g = {};
-  // the lines of the operand along which C is adjacent are the kernel's P
-  const bool row_major = c.cs == 1;
   g.P = row_major ? B.l : A.l;
   g.Q = row_major ? A.l : B.l;
   g.k = k;

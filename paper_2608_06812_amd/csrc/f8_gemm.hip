@@ -1,52 +1,9 @@
-// Matrix product of block-scaled 8-bit operands:
-//   C(p, q) = sum_b sP(p, b) sQ(q, b) sum_{k in b} P(p, k) Q(q, k)
-// over blocks b of 128, in FP32 (see f8_device.hpp for the two ways to the inner sums).
-// With scales in powers of two the whole sum stays in the matrix cores: an E8M0
-// scale is an operand of the 8-bit instruction, or of the conversion to BF16.
-// An FP32 scale multiplies a block's sum on its way into the FP32 accumulator.
-#include <type_traits>
-
-#include "f8_device.hpp"
+// The products of operands whose k values are adjacent (f8_gemm.hpp), and the
+// sum of k ranges.
+#include "f8_gemm.hpp"
 
 namespace ozfp4 {
 namespace {
-
-// Four values rounded to BF16 or FP16.
-__device__ __forceinline__ void narrow4(int type, v4f v, uint32_t (&w)[2]) {
-  if (type == OZFP4_BF16) {
-    typedef __bf16 h4 __attribute__((ext_vector_type(4)));
-    const h4 h = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-    __builtin_memcpy(w, &h, 8);
-  } else {
-    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-    const h4 h = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
-    __builtin_memcpy(w, &h, 8);
-  }
-}
-
-// Four adjacent elements, of which n exist, to C at `at`; vec: aligned for one
-// store.
-__device__ __forceinline__ void store4(void* C, int type, bool add, bool vec, int64_t at, v4f v, int n) {
-  if (type == OZFP4_F32) {
-    float* c = static_cast<float*>(C) + at;
-    if (n >= 4 && vec) {
-      v4f* c4 = reinterpret_cast<v4f*>(c);
-      *c4 = add ? *c4 + v : v;
-    } else {
-      for (int e = 0; e < 4; ++e)
-        if (e < n) c[e] = add ? c[e] + v[e] : v[e];
-    }
-    return;
-  }
-  uint32_t w[2];
-  narrow4(type, v, w);
-  uint16_t* c = static_cast<uint16_t*>(C) + at;
-  if (n >= 4 && vec)
-    *reinterpret_cast<uint2*>(c) = uint2{w[0], w[1]};
-  else
-    for (int e = 0; e < 4; ++e)
-      if (e < n) c[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-}
 
 // Memory bound: the partial sums once in, C once out.
 __global__ __launch_bounds__(256) void k_f8_sum(F8Sum s, bool vec) {
@@ -61,367 +18,12 @@ __global__ __launch_bounds__(256) void k_f8_sum(F8Sum s, bool vec) {
   }
 }
 
-// LDS DMA of one value of kSize bytes a lane, from base + offset to the word at
-// to + 4 lane (a byte is extended).
-template <int kSize>
-__device__ __forceinline__ void copy_words(const uint8_t* base, uint32_t offset, uint8_t* to) {
-  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, -1, kBufferWord3);
-  auto word = (__attribute__((address_space(3))) void*)to;
-  if constexpr (kSize == 1)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, word, 1, offset, 0, 0, 0);
-  else
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, word, 4, offset, 0, 0, 0);
-}
-
-// Block tile (WP TP 16) lines of P x (WQ TQ 16) of Q, a wave TP x TQ MFMA
-// tiles. A stage is one block of 128 of every line, 128 bytes a line, copied
-// into LDS by buffer-form LDS DMA into kSlots slots. A
-// copy is 8 lines; within a line the 16-byte piece c lies at c ^ (line / 2 % 8),
-// which the copy's lanes arrange by the addresses they read. An operand read
-// takes pieces g and g + 4 of line l % 16 in lane l = 16 g + ..., and the LDS
-// serves lanes 0-3, 12-15 and 20-27 together (then 4-11, 16-19 and 28-31, and
-// the upper half likewise): those fall on all 64 banks. (With pieces 2 g and
-// 2 g + 1 they fall on half of them, and half of the LDS cycles are conflicts.) The scales of a stage, one word a
-// line (a byte is extended on its way), are copied likewise.
-template <bool kExact, int kMode, int FP, int FQ, int WP, int WQ, int TP, int TQ, int kSlots>
-__global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned tiles_p, unsigned tiles_q) {
-  constexpr int kWavesN = WP * WQ;
-  constexpr int BP = WP * TP * 16, BQ = WQ * TQ * 16, kLines = BP + BQ;
-  constexpr int kBytes = kLines * kF8Block;
-  constexpr int CP = BP / 8 / kWavesN, CQ = BQ / 8 / kWavesN, kCopies = CP + CQ;   // per wave and stage
-  static_assert(CP % 2 == 0 && CQ % 2 == 0 && BP == 8 * kWavesN * CP && BQ == 8 * kWavesN * CQ, "whole pairs of copies a wave");
-  constexpr int kScaleCopies = (kLines / 64 + kWavesN - 1) / kWavesN, kPending = kCopies + kScaleCopies;
-  static_assert(kLines % 64 == 0 && BP % 64 == 0, "a copy of scales belongs to one operand");
-  static_assert(kSlots >= 2 && kSlots <= 4, "the waits for a stage");
-  constexpr int kScaleBytes = kScaleCopies * kWavesN * 256;
-  // one array: with two the compiler tells them apart, and waits for the copies
-  // in flight before every LDS read
-  __shared__ __align__(1024) uint8_t lds[kSlots * (kBytes + kScaleBytes)];
-  uint8_t* const scales = lds + kSlots * kBytes;
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wp = wave / WQ, wq = wave % WQ;
-  int range;
-  int64_t tp, tq;
-  tile_coords(blockIdx.x, gridDim.x, tiles_p, tiles_q, &range, &tp, &tq);
-  const int64_t p0 = tp * BP, q0 = tq * BQ;
-  const int total = (int)((g.k + kF8Block - 1) / kF8Block);
-  const int first = range * g.stages, nst = min(g.stages, total - first);
-  const int tail = (int)(g.k - (int64_t)(total - 1) * kF8Block);   // k values of the last stage
-
-  // this wave's copies: lines wave * C * 8 + 8 j + lane / 8 of each operand.
-  // Lines behind the last are read as the last (their results are not stored),
-  // pieces behind a line's end as its first (and left out of the products).
-  const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 4)) * 16;   // of even copies; of odd ones piece ^ 64
-  auto lines_from = [&](const F8Lines& l, int64_t line) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(l.x + line * l.ld), (short)0, -1, kBufferWord3);
-  };
-  const __amdgpu_buffer_rsrc_t from_p = lines_from(g.P, p0), from_q = lines_from(g.Q, q0);
-  const uint32_t ldp = (uint32_t)g.P.ld, ldq = (uint32_t)g.Q.ld;
-  const uint32_t last_p = (uint32_t)min(g.P.lines - 1 - p0, (int64_t)BP - 1) * ldp;
-  const uint32_t last_q = (uint32_t)min(g.Q.lines - 1 - q0, (int64_t)BQ - 1) * ldq;
-  const uint32_t own_p = (uint32_t)(wave * CP * 8 + (lane >> 3)) * ldp;
-  const uint32_t own_q = (uint32_t)(wave * CQ * 8 + (lane >> 3)) * ldq;
-  // and the scales of 64 lines (a wave with none of its own reads the last again)
-  constexpr int kScaleSize = kMode == kPow2 ? 1 : 4;
-  const uint8_t* scale_base[kScaleCopies];
-  int64_t scale_step[kScaleCopies];
-  uint32_t scale_own[kScaleCopies];
-#pragma unroll
-  for (int c = 0; c < kScaleCopies; ++c) {
-    const int line = min((c * kWavesN + wave) * 64, kLines - 64);   // the wave's first, BP on of Q
-    const bool of_p = line < BP;
-    const F8Lines& l = of_p ? g.P : g.Q;
-    const int64_t from = of_p ? p0 + line : q0 + (line - BP), end = l.lines - 1;
-    const int64_t base = min(from, end) >> l.shift;
-    scale_base[c] = static_cast<const uint8_t*>(l.s) + (base * l.sl + first * l.sk) * kScaleSize;
-    scale_step[c] = l.sk * kScaleSize;
-    scale_own[c] = (uint32_t)((min(from + lane, end) >> l.shift) - base) * (uint32_t)(l.sl * kScaleSize);
-  }
-  // copy n of stage s into its slot; every copy of a stage before the next stage's
-  auto copy = [&](int s, int n) {
-    const int st = first + s, slot = s % kSlots;
-    if (n < kCopies) {
-      const int end = st == total - 1 ? tail : kF8Block;
-      const uint32_t own = n % 2 ? piece ^ 64 : piece, at = (int)own < end ? own : 0;   // CP is even
-      uint8_t* to = lds + slot * kBytes;
-      if (n < CP)
-        dma16_buf(from_p, min(own_p + n * 8 * ldp, last_p) + at, (uint32_t)st * kF8Block, to + (wave * CP + n) * 1024);
-      else
-        dma16_buf(from_q, min(own_q + (n - CP) * 8 * ldq, last_q) + at, (uint32_t)st * kF8Block,
-                  to + (BP / 8 + wave * CQ + n - CP) * 1024);
-    } else {
-      const int c = n - kCopies;
-      copy_words<kScaleSize>(scale_base[c], scale_own[c], scales + slot * kScaleBytes + (c * kWavesN + wave) * 256);
-      scale_base[c] += scale_step[c];
-    }
-  };
-
-  v4f acc[TP][TQ];
-#pragma unroll
-  for (int i = 0; i < TP; ++i)
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-
-  // operand reads (any order of k will do, as long as both operands have it)
-  const int r = lane & 15, h = lane >> 4;
-  const int o0 = r * 128 + ((h ^ (r >> 1)) * 16), o1 = r * 128 + (((h + 4) ^ (r >> 1)) * 16);
-
-  // what has been read for the next tile of P and the next stage's Q (in the
-  // 8-bit form straight into the operands), with their scales
-  v8i raw_p, raw_q[kExact ? TQ : 1];
-  Frag<kExact> q[TQ];
-  uint32_t word_p = 0, word_q[TQ];
-  v4f line_p = {1, 1, 1, 1};
-  float tile_p = 1;
-  auto read = [&](const uint8_t* b) {
-    const v4i x = *reinterpret_cast<const v4i*>(b + o0), y = *reinterpret_cast<const v4i*>(b + o1);
-    return v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-  };
-  auto words = [&](int s) { return reinterpret_cast<const uint32_t*>(scales + (s % kSlots) * kScaleBytes); };
-  auto read_p = [&](int s, int i) {
-    raw_p = read(lds + (s % kSlots) * kBytes + (wp * TP + i) * 2048);
-    if constexpr (kMode == kPow2) word_p = words(s)[(wp * TP + i) * 16 + r];
-    if constexpr (kMode == kLineP)
-      line_p = *reinterpret_cast<const v4f*>(words(s) + (wp * TP + i) * 16 + (lane >> 4) * 4);
-    if constexpr (kMode == kTileP) {
-      if (i == 0) tile_p = __uint_as_float(words(s)[wp * TP * 16]);
-    }
-  };
-  auto read_q = [&](int s, int j) {
-    const v8i x = read(lds + (s % kSlots) * kBytes + BP * 128 + (wq * TQ + j) * 2048);
-    if constexpr (kExact)
-      raw_q[j] = x;
-    else
-      q[j].x = x;
-    word_q[j] = words(s)[BP + (wq * TQ + j) * 16 + r];
-  };
-
-  // a lane's values behind the end of the lines, in the last range's last stage
-  const int end = first + nst == total ? tail : kF8Block;
-  auto mask = [&](int e) -> uint32_t {
-    const int keep = end - (h * 16 + (e >> 2) * 64 + (e & 3) * 4);
-    return keep >= 4 ? ~0u : keep <= 0 ? 0u : (1u << (8 * keep)) - 1;
-  };
-  auto cut = [&](v8i x) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] &= (int)mask(e);
-    return x;
-  };
-
-  // Schedule. A tile of P meets the TQ tiles of Q one by one; with FP32 scales
-  // each product is scaled and added two products later, so that no addition
-  // waits for its product. The next tile of P is read a tile ahead. The handover
-  // to the next stage comes before a stage's last tile of P, whose operands are
-  // in registers by then: its products cover the barrier, the slot is free for
-  // the copies of the stage kSlots on, and each tile of Q is replaced by the
-  // next stage's as soon as its last product is issued. The copies are spread
-  // over the products, one for kEvery of them, from the handover on and into the
-  // next stage: a wave that issues all of them at once waits for the address
-  // unit, which takes 16 cycles a copy, and its products with it.
-  constexpr uint32_t one = 127;   // E8M0 1
-  constexpr int kUnits = TP * TQ;
-  constexpr int kPair = kExact ? 2 : 1;   // products whose instructions alternate
-  constexpr int kEvery = kExact || kUnits <= 16 ? 1 : 2;
-  constexpr int kAtOnce = kUnits <= 4 ? kPending : 0, kInLast = kAtOnce ? kAtOnce : TQ / kEvery;
-  static_assert(kInLast + (TP - 1) * TQ / kEvery >= kPending, "a stage's copies end before its handover");
-  static_assert(kUnits % 4 == 0 && TQ >= 2 && TP % 2 == 0, "products in flight are counted modulo 4");
-  v4f part[4] = {}, line[2] = {};
-  float factor[TQ], before[2] = {0, 0};
-#pragma unroll
-  for (int j = 0; j < TQ; ++j) factor[j] = 0;
-  // product u of a stage (one before its first: of the stage before)
-  auto add = [&](int u) {
-    const int v = (u + kUnits) % kUnits, i = v / TQ, j = v % TQ;
-    const float f = u < 0 ? before[j - (TQ - 2)] : factor[j];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      acc[i][j][e] = __builtin_fmaf(kMode == kLineP ? part[v % 4][e] * line[i & 1][e] : part[v % 4][e], f, acc[i][j][e]);
-  };
-
-  // Stage s, with kLeft = min(nst - s, kSlots + 1) stages left: the next one
-  // and the waits are known when the loop is compiled, since branches in a
-  // stage would let the compiler move its products behind the barrier.
-  auto stage = [&](int s, auto left) {
-    constexpr int kLeft = decltype(left)::value;
-    constexpr bool kMore = kLeft > 1;
-    constexpr int kUnderWay = kLeft > kSlots ? kSlots - 2 : kLeft - 2;   // stages copied behind the next one
-    if constexpr (kMode != kPow2) {
-      before[0] = factor[TQ - 2];
-      before[1] = factor[TQ - 1];
-#pragma unroll
-      for (int j = 0; j < TQ; ++j) factor[j] = tile_p * __uint_as_float(word_q[j]);
-    }
-    if constexpr (!kMore) {
-#pragma unroll
-      for (int j = 0; j < TQ; ++j) {
-        if constexpr (kExact)
-          raw_q[j] = cut(raw_q[j]);
-        else
-          q[j].x = cut(q[j].x);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < TP; ++i) {
-      const uint32_t e8 = kMode == kPow2 ? word_p : one;
-      const auto p = Frag<kExact>::template make<FP>(kMore ? raw_p : cut(raw_p), e8);
-      const v4f of_lines = line_p;
-      const bool last = i == TP - 1;
-      if (!last) {
-        read_p(s, i + 1);
-      } else if (kMore) {
-        // the next stage has landed, and every wave has read this one
-        wait_vm_lgkm0<(kMore ? kUnderWay * kPending : 0)>();
-        block_sync();
-        if (kAtOnce && kLeft > kSlots)
-#pragma unroll
-          for (int n = 0; n < kAtOnce; ++n) copy(s + kSlots, n);
-        read_p(s + 1, 0);
-      }
-#pragma unroll
-      for (int j0 = 0; j0 < TQ; j0 += kPair) {
-        if constexpr (kExact) {
-#pragma unroll
-          for (int j = j0; j < j0 + kPair; ++j)
-            if (i == 0) q[j] = Frag<kExact>::template make<FQ>(raw_q[j], kMode == kPow2 ? word_q[j] : one);
-        }
-#pragma unroll
-        for (int step = 0; step < Frag<kExact>::kSteps; ++step)
-#pragma unroll
-          for (int j = j0; j < j0 + kPair; ++j) {
-            v4f& c = kMode == kPow2 ? acc[i][j] : part[(i * TQ + j) % 4];
-            block_step<kMode == kPow2, FP, FQ>(p, q[j], step, c, kMode != kPow2 && step == 0, e8, word_q[j]);
-          }
-#pragma unroll
-        for (int j = j0; j < j0 + kPair; ++j) {
-          const int u = i * TQ + j;
-          if constexpr (kMode != kPow2) add(u - 2);
-          if (j == 1) line[i & 1] = of_lines;
-          if (last && kMore) read_q(s + 1, j);
-          if (!kAtOnce && last && kLeft > kSlots && j % kEvery == 0) copy(s + kSlots, j / kEvery);
-          if (!last && kLeft >= kSlots && u % kEvery == 0 && kInLast + u / kEvery < kPending)
-            copy(s + kSlots - 1, kInLast + u / kEvery);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  };
-  if (nst > 0) {
-    // the last slot's stage as far as a stage before it would have copied it
-#pragma unroll
-    for (int a = 0; a < kSlots; ++a)
-      if (a < nst)
-#pragma unroll
-        for (int n = 0; n < (a < kSlots - 1 ? kPending : kInLast); ++n) copy(a, n);
-    if (kSlots > 3 && nst > 3)
-      wait_vm_lgkm0<(kSlots > 3 ? 2 * kPending + kInLast : 0)>();
-    else if (kSlots > 2 && nst > 2)
-      wait_vm_lgkm0<(kSlots > 2 ? (kSlots > 3 ? 2 * kPending : kPending + kInLast) : 0)>();
-    else if (nst > 1)
-      wait_vm_lgkm0<(kSlots > 2 ? kPending : kInLast)>();
-    else
-      wait_vm_lgkm0<0>();
-    block_sync();
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) read_q(0, j);
-    read_p(0, 0);
-    int s = 0;
-    for (; nst - s > kSlots; ++s) stage(s, std::integral_constant<int, kSlots + 1>{});
-    if constexpr (kSlots > 3) {
-      if (nst - s == 4) stage(s++, std::integral_constant<int, 4>{});
-    }
-    if constexpr (kSlots > 2) {
-      if (nst - s == 3) stage(s++, std::integral_constant<int, 3>{});
-    }
-    if (nst - s == 2) stage(s++, std::integral_constant<int, 2>{});
-    stage(s, std::integral_constant<int, 1>{});
-  }
-  if constexpr (kMode != kPow2) {
-    add(kUnits - 2);
-    add(kUnits - 1);
-  }
-
-  const int64_t pw = p0 + wp * TP * 16, base = (int64_t)range * g.part;
-  if (g.vec8 && !g.partial && pw + TP * 16 <= g.P.lines) {
-    // 16-bit outputs: the words of two tiles change places between the rows of
-    // 16 lanes, so that a lane has eight adjacent lines and four lanes 64 bytes
-    // (with 8 bytes a lane the stores of 4096^2 outputs take 8.5 us, not XX)
-    const int at = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      const int64_t q = q0 + (wq * TQ + j) * 16 + r;
-#pragma unroll
-      for (int i = 0; i < TP; i += 2) {
-        uint32_t a[2], b[2];
-        narrow4(g.type, acc[i][j], a);
-        narrow4(g.type, acc[i + 1][j], b);
-        const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-        if (q < g.Q.lines)
-          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(g.C) + q * g.ldc + pw + i * 16 + at) =
-              uint4{(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < TQ; ++j) {
-    const int64_t q = q0 + (wq * TQ + j) * 16 + r;
-    if (q >= g.Q.lines) continue;
-#pragma unroll
-    for (int i = 0; i < TP; ++i) {
-      const int64_t p = pw + i * 16 + (lane >> 4) * 4, n = g.P.lines - p;
-      if (n > 0)
-        store4(g.C, g.partial ? OZFP4_F32 : g.type, g.accumulate, g.vec, base + q * g.ldc + p, acc[i][j],
-               n < 4 ? (int)n : 4);
-    }
-  }
-}
-
-template <bool kExact, int kMode, int FP, int FQ, int WP, int WQ, int TP, int TQ, int kSlots>
-hipError_t launch_tile(hipStream_t st, const F8Gemm& g) {
-  const int64_t tiles_p = (g.P.lines + WP * TP * 16 - 1) / (WP * TP * 16);
-  const int64_t tiles_q = (g.Q.lines + WQ * TQ * 16 - 1) / (WQ * TQ * 16);
-  const int64_t total = (g.k + kF8Block - 1) / kF8Block,
-                ranges = total > g.stages ? (total + g.stages - 1) / g.stages : 1;
-  hipLaunchKernelGGL((k_f8_gemm<kExact, kMode, FP, FQ, WP, WQ, TP, TQ, kSlots>), dim3((unsigned)(tiles_p * tiles_q * ranges)),
-                     dim3(WP * WQ * 64), 0, st, g, (unsigned)tiles_p, (unsigned)tiles_q);
-  return hipGetLastError();
-}
-
-template <bool kExact, int kMode, int FP, int FQ>
-hipError_t launch_size(hipStream_t st, const F8Gemm& g) {
-  switch (g.tile) {
-    case kF8Tile256:
-      if constexpr (kExact) return launch_tile<kExact, kMode, FP, FQ, 4, 2, 4, 4, 3>(st, g);
-      else return launch_tile<kExact, kMode, FP, FQ, 2, 4, 8, 4, 2>(st, g);
-    case kF8Tile128: return launch_tile<kExact, kMode, FP, FQ, 2, 2, 4, 4, 4>(st, g);
-    default: return launch_tile<kExact, kMode, FP, FQ, 2, 2, 2, 2, 4>(st, g);
-  }
-}
-
-template <bool kExact, int FP, int FQ>
-hipError_t launch_mode(hipStream_t st, const F8Gemm& g) {
-  if (g.pow2) return launch_size<kExact, kPow2, FP, FQ>(st, g);
-  if (g.P.shift) return launch_size<kExact, kTileP, FP, FQ>(st, g);
-  return launch_size<kExact, kLineP, FP, FQ>(st, g);
-}
-
-template <int FP, int FQ>
-hipError_t launch_formats(hipStream_t st, const F8Gemm& g) {
-  return g.type == OZFP4_F32 ? launch_mode<true, FP, FQ>(st, g) : launch_mode<false, FP, FQ>(st, g);
-}
-
 }  // namespace
 
+hipError_t launch_f8_gemm_turned(hipStream_t st, const F8Gemm& g);   // f8_gemm_turned.hip
+
 hipError_t launch_f8_gemm(hipStream_t st, const F8Gemm& g) {
-  switch (g.P.fmt * 2 + g.Q.fmt) {
-    case 0: return launch_formats<0, 0>(st, g);
-    case 1: return launch_formats<0, 1>(st, g);
-    case 2: return launch_formats<1, 0>(st, g);
-    default: return launch_formats<1, 1>(st, g);
-  }
+  return g.turned ? launch_f8_gemm_turned(st, g) : launch_gemm<false>(st, g);
 }
 
 hipError_t launch_f8_sum(hipStream_t st, const F8Sum& s) {

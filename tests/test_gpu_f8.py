@@ -254,6 +254,9 @@ def test_gemm_large(gpu_lib, dtype, kind):
     for m, n, k in ((3500, 3601, 300), (3585, 3590, 128), (4096, 3592, 515)):
         for a_tile, b_tile in ((False, True), (False, False), (True, False)):
             check_gemm(gpu_lib, operands(m, n, k, kind, E5, E4, a_tile, b_tile), dtype)
+    for m, n, k in ((3500, 3600, 300), (3600, 3488, 129), (2000, 2000, 640)):
+        check_gemm(gpu_lib, operands(m, n, k, kind, E5, E4, b_order="row"), dtype)
+        check_gemm(gpu_lib, operands(m, n, k, kind, E4, E5, b_tile=False, a_order="col", b_order="row"), dtype)
     room = torch.full((3503, 3611), 7.0, device="cuda", dtype=dtype)
     check_gemm(gpu_lib, operands(3500, 3601, 300, kind), dtype, out=room[1:3501, :3601])
     room[1:3501, :3601] = 7.0
@@ -277,7 +280,8 @@ def test_gemm_formats(gpu_lib, a_fmt, b_fmt, kind):
 def test_gemm_orders(gpu_lib, a_order, b_order):
     """Every storage order of the operands and of the output, aligned lines and
     others, new and given outputs."""
-    for m, n, k in ((5, 300, 256), (144, 160, 272), (131, 77, 259), (272, 16, 400), (9, 1024, 640)):
+    for m, n, k in ((5, 300, 256), (144, 160, 272), (131, 77, 259), (272, 16, 400), (9, 1024, 640), (80, 96, 128),
+                    (512, 96, 1101), (208, 208, 2048)):
         for kind in (F32, E8):
             ops = operands(m, n, k, kind, a_order=a_order, b_order=b_order)
             check_gemm(gpu_lib, ops, torch.bfloat16)
