@@ -111,6 +111,7 @@ struct F8Quantize {
   void* s0;
   int64_t s0l, s0k;
 };
-hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize& q);
+// One launch; two matrices (tiles of 128 x 128) are of one type and scale type.
+hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize* q, int count);
 
 }  // namespace ozfp4

@@ -212,8 +212,8 @@ Operand take_lines(Work& w, int64_t lines, int64_t k, int fmt, int pow2) {
   return o;
 }
 
-int quantize(hipStream_t st, const Source& X, int fmt, int pow2, int tile, const Operand* along_cols,
-             const Operand* along_rows) {
+F8Quantize quantize_of(const Source& X, int fmt, int pow2, int tile, const Operand* along_cols,
+                       const Operand* along_rows) {
   F8Quantize q = {};
   q.x = X.x;
   q.src = X.type;
@@ -241,8 +241,7 @@ int quantize(hipStream_t st, const Source& X, int fmt, int pow2, int tile, const
     q.s0l = o0->l.sl;
     q.s0k = o0->l.sk;
   }
-  F8_LAUNCH(launch_f8_quantize(st, q));
-  return OZFP4_OK;
+  return q;
 }
 
 int gemm(Work& w, int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A, const ozfp4_f8_matrix* B,
@@ -289,15 +288,16 @@ int linear(Work& w, int64_t m, int64_t n, int64_t k, const Source& X, int fmt, c
     rc = product(rest, nullptr, k, x, weights, pow2, y);
     if (rc) return rc;
     if (rest.used > w.bytes) return OZFP4_EWORKSPACE;
-    rc = quantize(library_stream(), X, fmt, pow2, 0, &x, nullptr);
-    if (rc) return rc;
+    const F8Quantize q = quantize_of(X, fmt, pow2, 0, &x, nullptr);
+    F8_LAUNCH(launch_f8_quantize(library_stream(), &q, 1));
   }
   return product(w, library_stream(), k, x, weights, pow2, y);
 }
 
 int backward(Work& w, int64_t m, int64_t n, int64_t k, const Source& dY, int dy_fmt, const Source& X, int x_fmt,
              const ozfp4_f8_matrix* W, int pow2, bool want_dx, const Out& dx, bool want_dw, const Out& dw) {
-  if (!dims_ok(m, n, k) || !tiles_ok(m, k, 64) || !tiles_ok(n, k, 64) || !tiles_ok(m, n, 128))
+  if (!dims_ok(m, n, k) || !tiles_ok(m, k, 64) || !tiles_ok(n, k, 64) || !tiles_ok(m, n, 128) ||
+      !tiles_ok(m, n + k, 128))
     return OZFP4_EINVAL;
   if (m > OZFP4_MAX_K_F8 || n > OZFP4_MAX_K_F8) return OZFP4_EKBOUND;
   int rc = check_matrix(W, n, k);
@@ -322,14 +322,12 @@ int backward(Work& w, int64_t m, int64_t n, int64_t k, const Source& dY, int dy_
     Work p = w;
     p.dry = !launch;
     if (launch) {
-      if (m > 0 && n > 0 && (want_dx || want_dw)) {
-        rc = quantize(st, dY, dy_fmt, pow2, 0, want_dx ? &dy1 : nullptr, want_dw ? &dy0 : nullptr);
-        if (rc) return rc;
-      }
-      if (m > 0 && k > 0 && want_dw) {
-        rc = quantize(st, X, x_fmt, pow2, 0, nullptr, &x0);
-        if (rc) return rc;
-      }
+      F8Quantize q[2];
+      int count = 0;
+      if (want_dx || want_dw)
+        q[count++] = quantize_of(dY, dy_fmt, pow2, 0, want_dx ? &dy1 : nullptr, want_dw ? &dy0 : nullptr);
+      if (want_dw) q[count++] = quantize_of(X, x_fmt, pow2, 0, nullptr, &x0);
+      F8_LAUNCH(launch_f8_quantize(st, q, count));
     }
     if (want_dx) {
       rc = product(p, st, n, dy1, cols_of(*W, k), pow2, dx);
@@ -387,8 +385,11 @@ int ozfp4_quantize_f8(int64_t rows, int64_t cols, const void* X, int x_type, int
     r = cols_of(*along_rows, cols);
   }
   const ozfp4_f8_matrix& any = along_cols ? *along_cols : *along_rows;
-  return quantize(library_stream(), Source{X, x_type, rows, cols, x_rs, x_cs}, any.format,
-                  scale_type == OZFP4_SCALE_E8M0, any.tile, along_cols ? &c : nullptr, along_rows ? &r : nullptr);
+  const F8Quantize q = quantize_of(Source{X, x_type, rows, cols, x_rs, x_cs}, any.format,
+                                   scale_type == OZFP4_SCALE_E8M0, any.tile, along_cols ? &c : nullptr,
+                                   along_rows ? &r : nullptr);
+  F8_LAUNCH(launch_f8_quantize(library_stream(), &q, 1));
+  return OZFP4_OK;
 }
 
 int ozfp4_gemm_f8(int64_t m, int64_t n, int64_t k, const ozfp4_f8_matrix* A, const ozfp4_f8_matrix* B,

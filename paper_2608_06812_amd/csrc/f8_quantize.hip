@@ -49,15 +49,12 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(F8Quantize p, int64_t 
 // LDS, where column c has 16 units of 8 rows, unit u at u ^ (c / 8): a wave's
 // writes then fall on all banks alike.
 template <int kSrc, bool kPow2, int kFmt, int kRows>
-__global__ __launch_bounds__(2048 / kRows) void k_f8_quantize(F8Quantize p, unsigned tiles_c) {
+__device__ __forceinline__ void quantize_tile(const F8Quantize& p, unsigned tr, unsigned tc, uint8_t* turned,
+                                              float (*colmax)[128], float* tilemax) {
   typedef typename Source<kSrc>::T T;
   constexpr int kThreads = 2048 / kRows, kWavesN = kThreads / 64;
-  __shared__ __align__(16) uint8_t turned[128 * 128];
-  __shared__ float colmax[kWavesN][128];
-  __shared__ float tilemax[kWavesN];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int cg = t & 15, rg = t >> 4;
-  const unsigned tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
   const int64_t row0 = (int64_t)tr * 128 + rg * kRows, col0 = (int64_t)tc * 128 + cg * 8;
 
   float x[kRows][8];
@@ -189,20 +186,39 @@ __global__ __launch_bounds__(2048 / kRows) void k_f8_quantize(F8Quantize p, unsi
   }
 }
 
+// Tiles of one matrix, or of two.
+struct F8QuantizeTiles {
+  F8Quantize q[2];
+  unsigned first, tiles_c[2];   // tiles of q[0]; tile columns of each
+};
+template <int kSrc, bool kPow2, int kRows>
+__global__ __launch_bounds__(2048 / kRows) void k_f8_quantize(F8QuantizeTiles two) {
+  __shared__ __align__(16) uint8_t turned[128 * 128];
+  __shared__ float colmax[32 / kRows][128];
+  __shared__ float tilemax[32 / kRows];
+  const bool second = blockIdx.x >= two.first;
+  const F8Quantize& p = two.q[second];
+  const unsigned b = blockIdx.x - (second ? two.first : 0), tiles_c = two.tiles_c[second];
+  const unsigned tr = b / tiles_c, tc = b - tr * tiles_c;
+  if (p.fmt == OZFP4_E4M3)
+    quantize_tile<kSrc, kPow2, OZFP4_E4M3, kRows>(p, tr, tc, turned, colmax, tilemax);
+  else
+    quantize_tile<kSrc, kPow2, OZFP4_E5M2, kRows>(p, tr, tc, turned, colmax, tilemax);
+}
+
+template <int kSrc, bool kPow2>
+hipError_t launch_tiles(hipStream_t st, const F8QuantizeTiles& two, unsigned count) {
+  // few tiles: four times the threads a tile, two rows each
+  if (count <= 512)
+    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, 2>), dim3(count), dim3(1024), 0, st, two);
+  else
+    hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, 8>), dim3(count), dim3(256), 0, st, two);
+  return hipGetLastError();
+}
+
 template <int kSrc, bool kPow2, int kFmt>
-hipError_t launch_format(hipStream_t st, const F8Quantize& q) {
-  const int64_t tr = (q.rows + 127) / 128, tc = (q.cols + 127) / 128;
-  if (q.q0 || q.tile) {
-    // few tiles: four times the threads a tile, two rows each
-    if (tr * tc <= 512)
-      hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt, 2>), dim3((unsigned)(tr * tc)), dim3(1024), 0, st, q,
-                         (unsigned)tc);
-    else
-      hipLaunchKernelGGL((k_f8_quantize<kSrc, kPow2, kFmt, 8>), dim3((unsigned)(tr * tc)), dim3(256), 0, st, q,
-                         (unsigned)tc);
-    return hipGetLastError();
-  }
-  const int64_t chunks = (tc + 15) / 16, most = std::max<int64_t>(1, (kLaunchThreads / 256) / chunks);
+hipError_t launch_rows(hipStream_t st, const F8Quantize& q) {
+  const int64_t chunks = (q.cols + 2047) / 2048, most = std::max<int64_t>(1, (kLaunchThreads / 256) / chunks);
   for (int64_t row = 0; row < q.rows; row += most)
     hipLaunchKernelGGL((k_f8_quantize_rows<kSrc, kPow2, kFmt>),
                        dim3((unsigned)(chunks * std::min(most, q.rows - row))), dim3(256), 0, st, q, row,
@@ -211,19 +227,34 @@ hipError_t launch_format(hipStream_t st, const F8Quantize& q) {
 }
 
 template <int kSrc, bool kPow2>
-hipError_t launch(hipStream_t st, const F8Quantize& q) {
-  return q.fmt == OZFP4_E4M3 ? launch_format<kSrc, kPow2, OZFP4_E4M3>(st, q)
-                             : launch_format<kSrc, kPow2, OZFP4_E5M2>(st, q);
+hipError_t launch(hipStream_t st, const F8Quantize* q, int count) {
+  if (count == 1 && !q->q0 && !q->tile)
+    return q->fmt == OZFP4_E4M3 ? launch_rows<kSrc, kPow2, OZFP4_E4M3>(st, *q)
+                                : launch_rows<kSrc, kPow2, OZFP4_E5M2>(st, *q);
+  F8QuantizeTiles two = {};
+  unsigned tiles = 0;
+  for (int i = 0; i < count; ++i) {
+    two.q[i] = q[i];
+    two.tiles_c[i] = (unsigned)((q[i].cols + 127) / 128);
+    tiles += (unsigned)((q[i].rows + 127) / 128) * two.tiles_c[i];
+    if (i == 0) two.first = tiles;
+  }
+  return launch_tiles<kSrc, kPow2>(st, two, tiles);
 }
 
 }  // namespace
 
-hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize& q) {
-  if (q.rows == 0 || q.cols == 0) return hipSuccess;
-  switch (q.src) {
-    case OZFP4_F32: return q.pow2 ? launch<OZFP4_F32, true>(st, q) : launch<OZFP4_F32, false>(st, q);
-    case OZFP4_BF16: return q.pow2 ? launch<OZFP4_BF16, true>(st, q) : launch<OZFP4_BF16, false>(st, q);
-    default: return q.pow2 ? launch<OZFP4_F16, true>(st, q) : launch<OZFP4_F16, false>(st, q);
+hipError_t launch_f8_quantize(hipStream_t st, const F8Quantize* q, int count) {
+  F8Quantize some[2];
+  int n = 0;
+  for (int i = 0; i < count; ++i)
+    if (q[i].rows > 0 && q[i].cols > 0) some[n++] = q[i];
+  if (n == 0) return hipSuccess;
+  const bool pow2 = some[0].pow2;
+  switch (some[0].src) {
+    case OZFP4_F32: return pow2 ? launch<OZFP4_F32, true>(st, some, n) : launch<OZFP4_F32, false>(st, some, n);
+    case OZFP4_BF16: return pow2 ? launch<OZFP4_BF16, true>(st, some, n) : launch<OZFP4_BF16, false>(st, some, n);
+    default: return pow2 ? launch<OZFP4_F16, true>(st, some, n) : launch<OZFP4_F16, false>(st, some, n);
   }
 }
 
