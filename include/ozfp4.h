@@ -225,7 +225,7 @@ int ozfp4_product(int op, int64_t m, int64_t n, int64_t k,
  * value (i, j) at values[i * rs + j * cs] (bytes; one stride is 1 and the
  * other at least the extent that runs along it), scale (i', j') at
  * scales[i' * srs + j' * scs] (in elements of the scale type, any strides
- * >= 0). Along the axis that a product sums over, a scale covers 128
+ * >= 0, at most 2^22 along the axis that a product does not sum over). Along the axis that a product sums over, a scale covers 128
  * elements (i' = i / 128 or j' = j / 128 there). Along the other it covers
  * one (tile = 0, a scale per line of 128) or 128 as well (tile = 1).
  */

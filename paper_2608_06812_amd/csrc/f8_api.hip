@@ -51,10 +51,12 @@ bool type_ok(int t) { return t >= OZFP4_F32 && t <= OZFP4_F16; }
 bool format_ok(int f) { return f == OZFP4_E4M3 || f == OZFP4_E5M2; }
 bool scale_ok(int s) { return s == OZFP4_SCALE_F32 || s == OZFP4_SCALE_E8M0; }
 
+bool scale_strides_ok(const ozfp4_f8_matrix& M) { return M.srs >= 0 && M.scs >= 0; }
+
 // A product's operand of the caller (rows x cols).
 int check_matrix(const ozfp4_f8_matrix* M, int64_t rows, int64_t cols) {
   if (!M || !format_ok(M->format) || (M->tile != 0 && M->tile != 1)) return OZFP4_EINVAL;
-  if (!layout_ok(rows, cols, M->rs, M->cs) || M->srs < 0 || M->scs < 0) return OZFP4_EINVAL;
+  if (!layout_ok(rows, cols, M->rs, M->cs) || !scale_strides_ok(*M)) return OZFP4_EINVAL;
   if (rows > 0 && cols > 0 && (!M->values || !M->scales)) return OZFP4_EINVAL;
   return OZFP4_OK;
 }
@@ -113,9 +115,12 @@ F8Token token_product(int64_t k, const Operand& few, const Operand& many, bool f
   return t;
 }
 
-// C = A B from the rows of A and the columns of B.
+// C = A B from the rows of A and the columns of B. A block tile's scale offsets
+// have to fit 32 bits.
+constexpr int64_t kMaxScaleStride = 1 << 22;
 int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, const Out& c) {
   if (A.l.lines == 0 || B.l.lines == 0 || (k == 0 && c.accumulate)) return OZFP4_OK;
+  if (A.l.sl > kMaxScaleStride || B.l.sl > kMaxScaleStride) return OZFP4_EINVAL;
   const bool few_rows = A.l.lines <= B.l.lines;
   const bool tokens = k > 0 && std::min(A.l.lines, B.l.lines) <= kF8TokenLines &&
                       std::max(A.l.lines, B.l.lines) <= kF8TokenMany;
@@ -357,7 +362,7 @@ int check_quantized(const ozfp4_f8_matrix& M, int64_t line_stride, int64_t k_str
   if (!format_ok(M.format) || (M.tile != 0 && M.tile != 1) || !M.values || !M.scales) return OZFP4_EINVAL;
   if (k_stride != 1 || line_stride < k || line_stride % 16 || reinterpret_cast<uintptr_t>(M.values) % 16)
     return OZFP4_EINVAL;
-  if (M.srs < 0 || M.scs < 0) return OZFP4_EINVAL;
+  if (!scale_strides_ok(M)) return OZFP4_EINVAL;
   return OZFP4_OK;
 }
 

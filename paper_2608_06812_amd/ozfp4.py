@@ -629,8 +629,10 @@ def _unit(X):
 def _source(X, name):
     """X with a unit stride (a row-major copy of any other layout), its type
     code and its strides."""
-    _device_matrix(X, name)
-    code = _code(_f8_types()[0], X.dtype, name)
+    code = (_f8_tables or _f8_types())[0].get(X.dtype) if hasattr(X, "dtype") else None
+    if code is None or not X.is_cuda or X.dim() != 2:   # say which
+        _device_matrix(X, name)
+        _code(_f8_types()[0], X.dtype, name)
     st = _unit(X)
     if st is None:
         X = X.contiguous()
@@ -639,33 +641,41 @@ def _source(X, name):
 
 
 def _quantized(Q, S, axis, name):
-    """F8Matrix of values Q and scales S along `axis`, the scale code, and the
-    values that back it."""
-    _device_matrix(Q, name)
-    _device_matrix(S, "S" + name)
-    _, formats, scales = _f8_types()
-    fmt = _code(formats, Q.dtype, name)
-    kind = _code(scales, S.dtype, "S" + name)
-    r, c = Q.shape
-    sr, sc = S.shape
-    br, bc = _blocks(r), _blocks(c)
-    if axis == 0:
-        lines = sr == br and sc == c
-    else:
-        lines = sr == r and sc == bc
+    """F8Matrix of values Q and scales S along `axis`, the scale code, the values
+    that back it, and their shape."""
+    _, formats, scales = _f8_tables or _f8_types()
+    try:
+        fmt, kind = formats[Q.dtype], scales[S.dtype]
+        r, c = Q.shape
+        sr, sc = S.shape
+        on_device = Q.is_cuda and S.is_cuda
+    except (AttributeError, KeyError, ValueError, TypeError):
+        on_device = False
+    if not on_device:   # say which
+        _device_matrix(Q, name)
+        _device_matrix(S, "S" + name)
+        _code(formats, Q.dtype, name)
+        _code(scales, S.dtype, "S" + name)
+    br, bc = (r + 127) >> 7, (c + 127) >> 7
+    lines = sr == br and sc == c if axis == 0 else sr == r and sc == bc
     if not lines and not (sr == br and sc == bc):
         raise ValueError(f"S{name} must have shape {(br, c) if axis == 0 else (r, bc)} or {(br, bc)}, not {(sr, sc)}")
-    st = _unit(Q)
-    if st is None:
-        Q = Q.contiguous()
+    rs, cs = Q.stride()
+    if not (r > 1 and c > 1 and ((cs == 1 and rs >= c) or (rs == 1 and cs >= r))):
         st = _unit(Q)
+        if st is None:
+            Q = Q.contiguous()
+            st = _unit(Q)
+        rs, cs = st
     srs, scs = S.stride()
-    return F8Matrix(Q.data_ptr(), st[0], st[1], S.data_ptr(), srs, scs, fmt, 0 if lines else 1), kind, Q
+    return F8Matrix(Q.data_ptr(), rs, cs, S.data_ptr(), srs, scs, fmt, 0 if lines else 1), kind, Q, r, c
 
 
 def _output(out, rows, cols, dtype, device, name):
     """`out` or a new row-major tensor, its type code and strides."""
-    code = _code(_f8_types()[0], dtype, f"{name}'s type")
+    code = (_f8_tables or _f8_types())[0].get(dtype)
+    if code is None:
+        _code(_f8_types()[0], dtype, f"{name}'s type")
     if out is None:
         return _th().empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device), code, (max(1, cols), 1)
     _device_matrix(out, name)
@@ -677,28 +687,25 @@ def _output(out, rows, cols, dtype, device, name):
     return out, code, st
 
 
-def _scratch(nbytes, device):
-    """(tensor, address) of a call's workspace. It comes from torch's
-    allocator: it belongs to the call's stream, or to the graph that the call
-    is captured into, and no two calls in flight share it."""
-    if nbytes == 0:
-        return None, None
-    T = _th().empty(nbytes, dtype=_th().uint8, device=device)
-    return T, T.data_ptr()
-
-
-def _run(tensors, fn, args, where):
-    """fn(*args) on the tensors' device and its current stream (see _on)."""
+def _run(tensors, fn, args, where, workspace=None):
+    """fn(*args) on the tensors' device and its current stream (see _on). With
+    `workspace`, a function that gives the bytes a call needs, fn's last two
+    arguments are a workspace, asked for when fn wants one. It comes from torch's
+    allocator: it belongs to the call's stream, or to the graph that the call is
+    captured into, and no two calls in flight share it."""
     dev = tensors[0].get_device()
     here = dev == _raw_device()
     for T in tensors:
         here = here and T.get_device() == dev
     if here:
         load().ozfp4_set_stream(_raw_stream(dev))
-        code = fn(*args)
+        code = fn(*args) if workspace is None else fn(*args, None, 0)
+        if code == OZFP4_EWORKSPACE:
+            ws = _th().empty(workspace(), dtype=_th().uint8, device=tensors[0].device)
+            code = fn(*args, ws.data_ptr(), ws.numel())
     else:
         with _on(tensors[0].device, *tensors):
-            code = fn(*args)
+            return _run(tensors, fn, args, where, workspace)
     _check(code, where)
 
 
@@ -767,10 +774,8 @@ def gemm_f8(A, SA, B, SB, out_dtype=None, out=None, accumulate: bool = False):
     is added to. Returns C (m x n), `out` or a new row-major tensor. Operands
     with k adjacent and lines 16-byte aligned, as quantize_f8 makes them, are
     read in place. Asynchronous; can be captured into a graph."""
-    a, kind, A = _quantized(A, SA, 1, "A")
-    b, kind_b, B = _quantized(B, SB, 0, "B")
-    m, k = A.shape
-    k2, n = B.shape
+    a, kind, A, m, k = _quantized(A, SA, 1, "A")
+    b, kind_b, B, k2, n = _quantized(B, SB, 0, "B")
     if k != k2:
         raise ValueError("inner dimensions differ")
     if kind != kind_b:
@@ -782,10 +787,9 @@ def gemm_f8(A, SA, B, SB, out_dtype=None, out=None, accumulate: bool = False):
     C, code, (rs, cs) = _output(out, m, n, out_dtype, A.device, "out")
     if accumulate and code != OZFP4_F32:
         raise TypeError("accumulate needs a float32 out")
-    ws, p = _scratch(ozfp4_gemm_f8_workspace(m, n, k, a, b, rs, cs), A.device)
     _run((A, SA, B, SB, C), load().ozfp4_gemm_f8,
-         (m, n, k, a, b, kind, C.data_ptr(), code, rs, cs, 1 if accumulate else 0, p, 0 if ws is None else ws.numel()),
-         "ozfp4_gemm_f8")
+         (m, n, k, a, b, kind, C.data_ptr(), code, rs, cs, 1 if accumulate else 0), "ozfp4_gemm_f8",
+         lambda: ozfp4_gemm_f8_workspace(m, n, k, a, b, rs, cs))
     return C
 
 
@@ -795,21 +799,18 @@ def linear_f8(X, W, SW, out_dtype=None, format=None, out=None):
     weights W (n x k) with scales SW along dimension 1. out_dtype defaults to
     X's type (or out's). Returns Y (m x n), `out` or a new row-major tensor.
     Asynchronous; can be captured into a graph."""
-    torch = _th()
-    w, kind, W = _quantized(W, SW, 1, "W")
-    fmt = _code(_f8_types()[1], torch.float8_e4m3fn if format is None else format, "format")
+    w, kind, W, n, k2 = _quantized(W, SW, 1, "W")
+    fmt = OZFP4_E4M3 if format is None else _code(_f8_types()[1], format, "format")
     X, x_code, (x_rs, x_cs) = _source(X, "X")
     m, k = X.shape
-    n, k2 = W.shape
     if k != k2:
         raise ValueError("inner dimensions differ")
     if out_dtype is None:
         out_dtype = X.dtype if out is None else out.dtype
     Y, code, (rs, cs) = _output(out, m, n, out_dtype, X.device, "out")
-    ws, p = _scratch(ozfp4_linear_f8_workspace(m, n, k, w, rs, cs), X.device)
     _run((X, W, SW, Y), load().ozfp4_linear_f8,
-         (m, n, k, X.data_ptr(), x_code, x_rs, x_cs, fmt, w, kind, Y.data_ptr(), code, rs, cs, p,
-          0 if ws is None else ws.numel()), "ozfp4_linear_f8")
+         (m, n, k, X.data_ptr(), x_code, x_rs, x_cs, fmt, w, kind, Y.data_ptr(), code, rs, cs), "ozfp4_linear_f8",
+         lambda: ozfp4_linear_f8_workspace(m, n, k, w, rs, cs))
     return Y
 
 
@@ -827,10 +828,9 @@ def linear_f8_backward(dY, X, W, SW, format=None, out_dtype=None, dX=None, dW=No
     formats = _f8_types()[1]
     fmt = _code(formats, e4m3 if format is None else format, "format")
     x_fmt = _code(formats, e4m3 if x_format is None else x_format, "x_format")
-    w, kind, W = _quantized(W, SW, 1, "W")
+    w, kind, W, n, k = _quantized(W, SW, 1, "W")
     dY, y_code, (y_rs, y_cs) = _source(dY, "dY")
     X, x_code, (x_rs, x_cs) = _source(X, "X")
-    n, k = W.shape
     m = X.shape[0]
     if X.shape[1] != k or tuple(dY.shape) != (m, n):
         raise ValueError("dY (m x n), X (m x k) and W (n x k) do not fit together")
@@ -845,11 +845,11 @@ def linear_f8_backward(dY, X, W, SW, format=None, out_dtype=None, dX=None, dW=No
     dX, code, (dx_rs, dx_cs) = _output(dX, m, k, out_dtype, X.device, "dX")
     dW, _, (dw_rs, dw_cs) = _output(dW, n, k, torch.float32, X.device, "dW")
     w.tile = 1
-    ws, p = _scratch(ozfp4_linear_f8_backward_workspace(m, n, k, w, dx_rs, dx_cs, dw_rs, dw_cs), X.device)
     _run((dY, X, W, SW, dX, dW), load().ozfp4_linear_f8_backward,
          (m, n, k, dY.data_ptr(), y_rs, y_cs, fmt, X.data_ptr(), x_rs, x_cs, x_fmt, x_code, w, kind,
-          dX.data_ptr(), code, dx_rs, dx_cs, dW.data_ptr(), dw_rs, dw_cs, 1 if accumulate else 0, p,
-          0 if ws is None else ws.numel()), "ozfp4_linear_f8_backward")
+          dX.data_ptr(), code, dx_rs, dx_cs, dW.data_ptr(), dw_rs, dw_cs, 1 if accumulate else 0),
+         "ozfp4_linear_f8_backward",
+         lambda: ozfp4_linear_f8_backward_workspace(m, n, k, w, dx_rs, dx_cs, dw_rs, dw_cs))
     return dX, dW
 
 

@@ -31,14 +31,15 @@ def gemm(m=70, n=80, k=256, A=None, B=None, kind=0, C=P, ctype=1, c_rs=80, c_cs=
     (dict(A=mat(255, 1)), EINVAL), (dict(A=mat(2, 2)), EINVAL), (dict(B=mat(1, 255)), EINVAL),
     (dict(A=mat(256, 1, fmt=2)), EINVAL), (dict(A=mat(256, 1, fmt=-1)), EINVAL),
     (dict(A=mat(256, 1, tile=2)), EINVAL), (dict(A=mat(256, 1, srs=-1)), EINVAL),
+    (dict(A=mat(256, 1, srs=(1 << 22) + 1)), EINVAL), (dict(B=mat(1, 256, scs=(1 << 22) + 1)), EINVAL),
     (dict(A=mat(256, 1, values=None)), EINVAL), (dict(B=mat(1, 256, scales=None)), EINVAL),
     (dict(A=ctypes.POINTER(ozfp4.F8Matrix)()), EINVAL),
     (dict(kind=2), EINVAL), (dict(kind=-1), EINVAL), (dict(C=None), EINVAL),
     (dict(ctype=3), EINVAL), (dict(ctype=-1), EINVAL), (dict(c_rs=79), EINVAL), (dict(c_rs=2, c_cs=2), EINVAL),
     (dict(add=1), EINVAL), (dict(add=1, ctype=2), EINVAL),
     (dict(ws=P + 64, nbytes=1 << 20), EINVAL),
-    (dict(A=mat(257, 1)), EWS), (dict(B=mat(80, 1)), EWS), (dict(A=mat(256, 1, values=P + 1)), EWS),
-    (dict(B=mat(80, 1), ws=P, nbytes=80 * 256 - 1), EWS),
+    (dict(A=mat(257, 1)), EWS), (dict(B=mat(88, 1)), EWS), (dict(A=mat(256, 1, values=P + 1)), EWS),
+    (dict(B=mat(88, 1), ws=P, nbytes=80 * 256 - 1), EWS),
     (dict(m=0), 0), (dict(n=0), 0), (dict(k=0, A=mat(1, 1), B=mat(1, 1), ctype=0, add=1), 0),
 ])
 def test_gemm_refusals(kw, code):
@@ -46,14 +47,16 @@ def test_gemm_refusals(kw, code):
 
 
 def test_workspace_sizes():
-    """Nothing for operands that are read in place, the packed lines of the
-    others (beside few lines on the other side only those whose k values are
-    not adjacent)."""
+    """Nothing for operands that are read in place (the one along which C is
+    adjacent in either order), the packed lines of the others (beside few lines
+    on the other side only those whose k values are not adjacent)."""
     ask = lambda A, B, n=80: ozfp4.ozfp4_gemm_f8_workspace(100, n, 300, A, B, n, 1)
     assert ask(mat(304, 1), mat(1, 304)) == 0
     assert ask(mat(300, 1), mat(1, 304)) == 100 * 384
-    assert ask(mat(304, 1), mat(80, 1)) == 80 * 384
-    assert ask(mat(1, 100), mat(80, 1)) == 180 * 384
+    assert ask(mat(304, 1), mat(80, 1)) == 0
+    assert ask(mat(304, 1), mat(88, 1)) == 80 * 384
+    assert ask(mat(1, 100), mat(80, 1)) == 100 * 384
+    assert ask(mat(1, 112), mat(88, 1)) == 180 * 384
     assert ask(mat(300, 1), mat(1, 301), 60) == 0
     assert ask(mat(300, 1), mat(60, 1), 60) == 60 * 384
     assert ask(mat(304, 1, values=P + 8), mat(1, 304)) == 100 * 384
