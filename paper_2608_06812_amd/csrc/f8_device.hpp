@@ -26,27 +26,57 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 enum F8Mode { kPow2, kTileP, kLineP };   // E8M0; FP32 with one scale per 128 lines of P; FP32 per line
 
+// 16 bytes at any address, as the dwords that hold them: the memory pipeline
+// takes an odd address apart (2.5 times the time of a kernel that only reads).
+// No dword without a byte of the 16 is read.
+struct Dwords {
+  v4i x;
+  int y;
+  uint32_t shift;   // bytes
+  __device__ __forceinline__ v4i bytes() const {
+    return v4i{(int)__builtin_amdgcn_alignbyte(x.y, x.x, shift), (int)__builtin_amdgcn_alignbyte(x.z, x.y, shift),
+               (int)__builtin_amdgcn_alignbyte(x.w, x.z, shift), (int)__builtin_amdgcn_alignbyte(y, x.w, shift)};
+  }
+};
+__device__ __forceinline__ Dwords load_dwords(const uint8_t* p) {
+  Dwords d;
+  d.shift = (uint32_t)reinterpret_cast<uintptr_t>(p) & 3;
+  const int* at = reinterpret_cast<const int*>(p - d.shift);
+  __builtin_memcpy(&d.x, __builtin_assume_aligned(at, 4), 16);
+  d.y = at[d.shift ? 4 : 3];
+  return d;
+}
+
+// 16 bytes moved down by 16 - n, 0 < n < 16, zeros behind them.
+__device__ __forceinline__ v4i last_bytes(v4i v, int n) {
+  uint64_t w[2];
+  __builtin_memcpy(w, &v, 16);
+  const int bits = 8 * (16 - n);
+  w[0] = bits >= 64 ? w[1] >> (bits - 64) : w[0] >> bits | w[1] << (64 - bits);
+  w[1] = bits >= 64 ? 0 : w[1] >> bits;
+  __builtin_memcpy(&v, w, 16);
+  return v;
+}
+
 // The n < 16 last bytes of a line that starts at `line` (n <= 0: none), from p
 // on, and zeros: the 16 bytes that end with the line, moved down, or one by one
 // where the line is shorter than that.
 __device__ __forceinline__ v4i load_end(const uint8_t* line, const uint8_t* p, int n) {
-  uint64_t w[2] = {0, 0};
+  v4i v = {0, 0, 0, 0};
   if (n > 0) {
     if (p + n - line >= 16) {
-      __builtin_memcpy(w, p + n - 16, 16);
-      const int bits = 8 * (16 - n);
-      w[0] = bits >= 64 ? w[1] >> (bits - 64) : w[0] >> bits | w[1] << (64 - bits);
-      w[1] = bits >= 64 ? 0 : w[1] >> bits;
+      __builtin_memcpy(&v, p + n - 16, 16);
+      v = last_bytes(v, n);
     } else {
+      uint64_t w[2] = {0, 0};
 #pragma unroll 1
       for (int e = n - 1; e >= 0; --e) {
         w[1] = w[1] << 8 | w[0] >> 56;
         w[0] = w[0] << 8 | p[e];
       }
+      __builtin_memcpy(&v, w, 16);
     }
   }
-  v4i v;
-  __builtin_memcpy(&v, w, 16);
   return v;
 }
 

@@ -26,24 +26,27 @@ __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
   const int64_t l0 = (int64_t)(b % nl) * kPackTile, k0 = (int64_t)(b / nl) * kPackTile;
   const int t = threadIdx.x, sub = t & 31, row = t >> 5;   // 4 bytes of a row of the tile, 8 rows a pass
   if (p.ks == 1) {
-    uint4 w[4];
+    // all loads before the first use, those of a line's end too: the 16 bytes
+    // that end with it
+    Dwords d[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
-      w[n] = uint4{0, 0, 0, 0};
-      if (line >= p.lines || kk >= p.k) continue;
-      const uint8_t* src = p.x + line * p.ls + kk;
-      if (kk + 16 <= p.k) {
-        __builtin_memcpy(&w[n], src, 16);
-      } else {
-        const v4i v = load_end(src - kk, src, (int)(p.k - kk));
-        __builtin_memcpy(&w[n], &v, 16);
-      }
+      if (line < p.lines && kk < p.k && p.k >= 16) d[n] = load_dwords(p.x + line * p.ls + min(kk, p.k - 16));
     }
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
-      if (line < p.lines && kk < p.k) *reinterpret_cast<uint4*>(p.out + line * p.ld + kk) = w[n];
+      if (line >= p.lines || kk >= p.k) continue;
+      v4i v;
+      if (p.k >= 16) {
+        v = d[n].bytes();
+        if (kk + 16 > p.k) v = last_bytes(v, (int)(p.k - kk));
+      } else {
+        const uint8_t* from = p.x + line * p.ls;
+        v = load_end(from, from + kk, (int)(p.k - kk));
+      }
+      *reinterpret_cast<v4i*>(p.out + line * p.ld + kk) = v;
     }
     return;
   }

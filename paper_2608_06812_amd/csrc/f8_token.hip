@@ -23,22 +23,38 @@ namespace {
 
 constexpr int kTokWaves = 8;
 
-// The 32 values of lane group g in the block that starts at byte `at` of a line:
-// 16-byte pieces g and g + 4, of which `left` bytes exist (kWhole: all). Any
-// alignment.
-template <bool kWhole>
-__device__ __forceinline__ v8i load_block(const uint8_t* line, int64_t at, int g, int left) {
+// The 32 values of lane group g in a block: 16-byte pieces g and g + 4, from
+// aligned lines (every line at a multiple of 4 bytes) or, kAny, any others.
+template <bool kAny> struct Values;
+template <> struct Values<false> {
   v4i v[2];
+  __device__ __forceinline__ void load(int h, const uint8_t* p) { __builtin_memcpy(&v[h], __builtin_assume_aligned(p, 4), 16); }
+  __device__ __forceinline__ void set(int h, v4i x) { v[h] = x; }
+  __device__ __forceinline__ v8i get() const { return v8i{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w}; }
+};
+template <> struct Values<true> {
+  Dwords v[2];
+  __device__ __forceinline__ void load(int h, const uint8_t* p) { v[h] = load_dwords(p); }
+  __device__ __forceinline__ void set(int h, v4i x) { v[h] = Dwords{x, 0, 0}; }
+  __device__ __forceinline__ v8i get() const {
+    const v4i a = v[0].bytes(), b = v[1].bytes();
+    return v8i{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  }
+};
+
+// Those of the block that starts at byte `at` of a line, of which `left` bytes
+// exist (kWhole: all).
+template <bool kWhole, bool kAny>
+__device__ __forceinline__ void load_block(Values<kAny>& v, const uint8_t* line, int64_t at, int g, int left) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int c = (g + 4 * h) * 16;
     const uint8_t* p = line + at + c;
     if (kWhole || c + 16 <= left)
-      __builtin_memcpy(&v[h], p, 16);
+      v.load(h, p);
     else
-      v[h] = load_end(line, p, left - c);
+      v.set(h, load_end(line, p, left - c));
   }
-  return v8i{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 }
 
 template <bool kPow2>
@@ -84,7 +100,7 @@ __device__ __forceinline__ void quantize_tokens(const F8Token& t, int m, int tot
 // A block: 16 TP lines of P, all lines of Q (16 TQ at most). The tokens are
 // the rows of the matrix instruction and the lines of P its columns, so that a
 // lane needs one scale of P a tile, whether that is a line's or a tile's.
-template <bool kPow, int TP, int TQ, int kSrc>
+template <bool kPow, bool kAny, int TP, int TQ, int kSrc>
 __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_token(F8Token t) {
   constexpr bool kFused = kSrc >= 0;
   constexpr int kDeep = 2;              // blocks of 128 in flight in a wave
@@ -117,17 +133,17 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
   }
 
   struct Stage {
-    v8i p[TP], q[TQ];
+    Values<kAny> p[TP], q[TQ];
     uint32_t sp[TP], sq[TQ];
   };
   auto fetch = [&](int s, Stage& f) {
     const int64_t at = (int64_t)s * kF8Block;
     auto blocks = [&](auto whole, int left) {
 #pragma unroll
-      for (int i = 0; i < TP; ++i) f.p[i] = load_block<decltype(whole)::value>(px[i], at, g, left);
+      for (int i = 0; i < TP; ++i) load_block<decltype(whole)::value>(f.p[i], px[i], at, g, left);
       if constexpr (!kFused) {
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) f.q[j] = load_block<decltype(whole)::value>(qx[j], at, g, left);
+        for (int j = 0; j < TQ; ++j) load_block<decltype(whole)::value>(f.q[j], qx[j], at, g, left);
       }
     };
     if (s == total - 1 && tail < kF8Block)
@@ -174,7 +190,8 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
           const uint8_t* b = lds + (s * m + lq[j]) * 128;
           const v4i x = *reinterpret_cast<const v4i*>(b + ((g ^ (lq[j] & 7)) * 16));
           const v4i y = *reinterpret_cast<const v4i*>(b + (((g + 4) ^ (lq[j] & 7)) * 16));
-          f.q[j] = v8i{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+          f.q[j].set(0, x);
+          f.q[j].set(1, y);
           f.sq[j] = held[s * m + lq[j]];
         }
       }
@@ -185,8 +202,8 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
 #pragma unroll
           for (int v = 0; v < 4; ++v) sq[j][v] = __shfl(__uint_as_float(f.sq[j]), g * 4 + v);
       }
-      auto as_p = [&](int i) { return to_bf16(f.p[i], kPow ? f.sp[i] : one, t.P.fmt); };
-      auto as_q = [&](int j) { return to_bf16(f.q[j], kPow ? f.sq[j] : one, t.Q.fmt); };
+      auto as_p = [&](int i) { return to_bf16(f.p[i].get(), kPow ? f.sp[i] : one, t.P.fmt); };
+      auto as_q = [&](int j) { return to_bf16(f.q[j].get(), kPow ? f.sq[j] : one, t.Q.fmt); };
       auto add = [&](int i, int j, const Frag<true>& p, const Frag<true>& q) {
         if constexpr (kPow) {
           acc[i][j] = block_product(q, p, acc[i][j]);
@@ -254,22 +271,30 @@ __global__ __launch_bounds__(kTokWaves * 64, TP + TQ == 2 ? 4 : 2) void k_f8_tok
   }
 }
 
-template <bool kPow, int TP, int TQ, int kSrc>
+template <bool kPow, bool kAny, int TP, int TQ, int kSrc>
 hipError_t launch(hipStream_t st, const F8Token& t) {
-  hipLaunchKernelGGL((k_f8_token<kPow, TP, TQ, kSrc>), dim3((unsigned)((t.P.lines + 16 * TP - 1) / (16 * TP))),
+  hipLaunchKernelGGL((k_f8_token<kPow, kAny, TP, TQ, kSrc>), dim3((unsigned)((t.P.lines + 16 * TP - 1) / (16 * TP))),
                      dim3(kTokWaves * 64), 0, st, t);
   return hipGetLastError();
 }
 
-// Lines of P a block takes: as many as leave about a block a CU, since every
-// block reads all lines of Q.
+// Lines of P a block takes: as many as leave about a block a CU where there are
+// more than 16 tokens, since every block reads all of them (24 tokens, 16384
+// lines of 4096: 27 us with 16 lines, 16.7 with 64); for fewer tokens more blocks
+// are better (one token, 8192 lines of 8192: 14.3 us with 16, 19 with 32). 64
+// lines need more registers than FP32 scales or unaligned lines leave.
 template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
+  auto aligned = [](const F8Lines& l) { return (reinterpret_cast<uintptr_t>(l.x) | (l.lines > 1 ? l.ld : 0)) % 4 == 0; };
+  const bool any = !aligned(t.P) || (kSrc < 0 && !aligned(t.Q));
   if constexpr (TQ == 2) {
-    if (kPow && t.P.lines >= 4 * 16 * 256) return launch<kPow, 4, TQ, kSrc>(st, t);   // FP32 scales: no registers
-    if (t.P.lines >= 2 * 16 * 256) return launch<kPow, 2, TQ, kSrc>(st, t);
+    if constexpr (kPow) {
+      if (!any && t.P.lines >= 4 * 16 * 256) return launch<kPow, false, 4, TQ, kSrc>(st, t);
+    }
+    if (t.P.lines >= 2 * 16 * 256)
+      return any ? launch<kPow, true, 2, TQ, kSrc>(st, t) : launch<kPow, false, 2, TQ, kSrc>(st, t);
   }
-  return launch<kPow, 1, TQ, kSrc>(st, t);
+  return any ? launch<kPow, true, 1, TQ, kSrc>(st, t) : launch<kPow, false, 1, TQ, kSrc>(st, t);
 }
 
 template <bool kPow>

@@ -57,8 +57,8 @@ def test_workspace_sizes():
     assert ask(mat(304, 1), mat(88, 1)) == 80 * 384
     assert ask(mat(1, 100), mat(80, 1)) == 100 * 384
     assert ask(mat(1, 112), mat(88, 1)) == 180 * 384
-    assert ask(mat(300, 1), mat(1, 301), 60) == 0
-    assert ask(mat(300, 1), mat(60, 1), 60) == 60 * 384
+    assert ask(mat(300, 1), mat(1, 301), 30) == 0
+    assert ask(mat(300, 1), mat(30, 1), 30) == 30 * 384
     assert ask(mat(304, 1, values=P + 8), mat(1, 304)) == 100 * 384
     with pytest.raises(ozfp4.OzFP4Error):
         ask(mat(10, 1), mat(1, 304))
