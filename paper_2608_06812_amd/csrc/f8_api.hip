@@ -121,11 +121,20 @@ constexpr int64_t kMaxScaleStride = 1 << 22;
 int product(Work& w, hipStream_t st, int64_t k, Operand A, Operand B, int pow2, const Out& c) {
   if (A.l.lines == 0 || B.l.lines == 0 || (k == 0 && c.accumulate)) return OZFP4_OK;
   if (A.l.sl > kMaxScaleStride || B.l.sl > kMaxScaleStride) return OZFP4_EINVAL;
-  const bool few_rows = A.l.lines <= B.l.lines;
-  const bool tokens = k > 0 && std::min(A.l.lines, B.l.lines) <= kF8TokenLines &&
-                      std::max(A.l.lines, B.l.lines) <= kF8TokenMany;
-  // the lines of the operand along which C is adjacent are the kernel's P
-  const bool row_major = c.cs == 1;
+  // the lines of the operand along which C is adjacent are the GEMM's P
+  const bool row_major = c.cs == 1, few_rows = A.l.lines <= B.l.lines;
+  const Operand& many = few_rows ? B : A;
+  // Few tokens take the kernel that reads lines of k, unless the GEMM's 64 x 64
+  // tiles read operands in place and are faster: weights with their lines
+  // adjacent (24 tokens, 16384 lines of 4096: 14.7 us, with a relayout 47), and
+  // more than 8 tokens with weights of 32 MiB on (token kernel / GEMM, us, 16-bit
+  // output: 16384 lines of 4096 and 8, 16, 32 tokens 16.6 / 15.6, 18.2 / 12.8, 21.5
+  // / 12.8; 8192 of 8192 16.4 / 16.4, 18.9 / 16.7, 20.6 / 17.4; 4096 of 4096 6.0 /
+  // 9.3, 6.7 / 9.8, 8.9 / 10.7; FP32 output, 8192 of 8192 and 32: 20.4 / 20.5).
+  const int64_t least = std::min(A.l.lines, B.l.lines), most = std::max(A.l.lines, B.l.lines);
+  const bool turned = many.ks != 1 && k > 1 && row_major == few_rows && in_place_turned(many);
+  const bool large = least > 8 && most * k >= kF8TokenBytes && in_place(A, k) && in_place(B, k);
+  const bool tokens = k > 0 && !turned && !large && least <= kF8TokenLines && most <= kF8TokenMany;
   F8Gemm g = {};
   F8Pack pack[2];
   int packs = 0;

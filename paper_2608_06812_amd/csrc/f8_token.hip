@@ -278,19 +278,14 @@ hipError_t launch(hipStream_t st, const F8Token& t) {
   return hipGetLastError();
 }
 
-// Lines of P a block takes: as many as leave about a block a CU where there are
-// more than 16 tokens, since every block reads all of them (24 tokens, 16384
-// lines of 4096: 27 us with 16 lines, 16.7 with 64); for fewer tokens more blocks
-// are better (one token, 8192 lines of 8192: 14.3 us with 16, 19 with 32). 64
-// lines need more registers than FP32 scales or unaligned lines leave.
+// Lines of P a block takes: for more than 16 tokens as many as leave about a
+// block a CU, since every block reads all of the tokens; for fewer more blocks
+// are better (one token, 8192 lines of 8192: 14.3 us with 16 lines, 19 with 32).
 template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
   auto aligned = [](const F8Lines& l) { return (reinterpret_cast<uintptr_t>(l.x) | (l.lines > 1 ? l.ld : 0)) % 4 == 0; };
   const bool any = !aligned(t.P) || (kSrc < 0 && !aligned(t.Q));
   if constexpr (TQ == 2) {
-    if constexpr (kPow) {
-      if (!any && t.P.lines >= 4 * 16 * 256) return launch<kPow, false, 4, TQ, kSrc>(st, t);
-    }
     if (t.P.lines >= 2 * 16 * 256)
       return any ? launch<kPow, true, 2, TQ, kSrc>(st, t) : launch<kPow, false, 2, TQ, kSrc>(st, t);
   }

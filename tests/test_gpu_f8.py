@@ -237,7 +237,8 @@ def check_gemm(lib, ops, out_dtype=torch.float32, out=None, accumulate=False):
 SIZES = [(1, 1, 1), (1, 128, 128), (2, 3, 5), (16, 16, 128), (17, 33, 129), (64, 64, 256), (65, 130, 384),
          (100, 1, 300), (1, 100, 300), (128, 128, 15), (256, 256, 512), (257, 255, 640), (300, 500, 1000),
          (48, 700, 144), (513, 129, 131), (40, 1040, 1300), (2, 5000, 1024),
-         (5000, 30, 1111), (64, 3000, 2048), (20, 17000, 515), (3, 9000, 1021), (31, 40, 2049)]
+         (5000, 30, 1111), (64, 3000, 2048), (20, 17000, 515), (3, 9000, 1021), (31, 40, 2049),
+         (20, 17000, 2000), (17000, 9, 2000)]
 
 
 @pytest.mark.parametrize("kind", [F32, E8])
