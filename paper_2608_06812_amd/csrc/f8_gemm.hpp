@@ -1,6 +1,7 @@
 // Matrix product of block-scaled 8-bit operands:
 //   C(p, q) = sum_b sP(p, b) sQ(q, b) sum_{k in b} P(p, k) Q(q, k)
-// over blocks b of 128, in FP32 (see f8_device.hpp for the two ways to the inner sums).
+// over blocks b of 128, in FP32 (see f8_device.hpp for the two ways to the inner
+// sums).
 // With scales in powers of two the whole sum stays in the matrix cores: an E8M0
 // scale is an operand of the 8-bit instruction, or of the conversion to BF16.
 // An FP32 scale multiplies a block's sum on its way into the FP32 accumulator.
@@ -61,6 +62,7 @@ __device__ __forceinline__ void copy_words(const uint8_t* base, uint32_t offset,
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, word, 4, offset, 0, 0, 0);
 }
 
+// Where a row's 16-byte pieces lie in LDS (kTurned below).
 template <int BP>
 __device__ __forceinline__ int turn(int k) {
   if constexpr (BP == 256) return (k & 7) | (k >> 4 & 1) << 3;
@@ -90,14 +92,25 @@ __device__ __forceinline__ v8i read_turned(const uint8_t* from) {
 
 // Block tile (WP TP 16) lines of P x (WQ TQ 16) of Q, a wave TP x TQ MFMA
 // tiles. A stage is one block of 128 of every line, 128 bytes a line, copied
-// into LDS by buffer-form LDS DMA into kSlots slots. A
-// copy is 8 lines; within a line the 16-byte piece c lies at c ^ (line / 2 % 8),
-// which the copy's lanes arrange by the addresses they read. An operand read
-// takes pieces g and g + 4 of line l % 16 in lane l = 16 g + ..., and the LDS
-// serves lanes 0-3, 12-15 and 20-27 together (then 4-11, 16-19 and 28-31, and
-// the upper half likewise): those fall on all 64 banks. (With pieces 2 g and
-// 2 g + 1 they fall on half of them, and half of the LDS cycles are conflicts.) The scales of a stage, one word a
-// line (a byte is extended on its way), are copied likewise.
+// into LDS by buffer-form LDS DMA into kSlots slots. A copy is 8 lines; within a
+// line the 16-byte piece c lies at c ^ (line / 2 % 8), which the copy's lanes
+// arrange by the addresses they read. An operand read takes pieces g and g + 4 of
+// line l % 16 in lane l = 16 g + ..., and the LDS serves lanes 0-3, 12-15 and
+// 20-27 together (then 4-11, 16-19 and 28-31, and the upper half likewise): those
+// fall on all 64 banks. (With pieces 2 g and 2 g + 1 they fall on half of them,
+// and half of the LDS cycles are conflicts: 8192^3 479 us in place of 466.) The
+// scales of a stage, one word a line (a byte is extended on its way), are copied
+// likewise.
+//
+// 256 x 256 tiles with two slots, for outputs of 16 bits, need 16 bytes of
+// operands a cycle and CU; 256 x 128 with three, where the BF16 form takes twice
+// the matrix cycles, as many. At 8192^3 they keep the matrix cores 68 % busy (BF16
+// 69 %) at 1.74 GHz (2.1), where the power limit holds the chip: 2.50 PFLOP/s with
+// FP32 scales, 2.77 with powers of two, and 1.16 and 1.25 to FP32, beside 2.82 and
+// 1.31 of the library's products with one scale for all. A weight gradient with a
+// scale a line on both sides (4096 x 4096 x 16384: 1.05 PFLOP/s) is bound by the
+// vector instructions that scale and convert: 70 % of the issue cycles beside 49 %
+// of the matrix cores'.
 //
 // kTurned: P's lines are adjacent where its k values would be (the weights of a
 // layer in the product with an output gradient): rows of k, P.ld bytes apart. A
@@ -111,7 +124,8 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   constexpr int BP = WP * TP * 16, BQ = WQ * TQ * 16, kLines = BP + BQ;
   constexpr int kBytes = kLines * kF8Block;
   constexpr int CP = BP / 8 / kWavesN, CQ = BQ / 8 / kWavesN, kCopies = CP + CQ;   // per wave and stage
-  static_assert(CP % 2 == 0 && CQ % 2 == 0 && BP == 8 * kWavesN * CP && BQ == 8 * kWavesN * CQ, "whole pairs of copies a wave");
+  static_assert(CP % 2 == 0 && CQ % 2 == 0 && BP == 8 * kWavesN * CP && BQ == 8 * kWavesN * CQ,
+                "whole pairs of copies a wave");
   constexpr int kScaleCopies = (kLines / 64 + kWavesN - 1) / kWavesN, kPending = kCopies + kScaleCopies;
   static_assert(kLines % 64 == 0 && BP % 64 == 0, "a copy of scales belongs to one operand");
   static_assert(kSlots >= 2 && kSlots <= 4, "the waits for a stage");
@@ -274,7 +288,8 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
     const float f = u < 0 ? before[j - (TQ - 2)] : factor[j];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      acc[i][j][e] = __builtin_fmaf(kMode == kLineP ? part[v % 4][e] * line[i & 1][e] : part[v % 4][e], f, acc[i][j][e]);
+      acc[i][j][e] =
+          __builtin_fmaf(kMode == kLineP ? part[v % 4][e] * line[i & 1][e] : part[v % 4][e], f, acc[i][j][e]);
   };
 
   // Stage s, with kLeft = min(nst - s, kSlots + 1) stages left: the next one
@@ -383,7 +398,7 @@ __global__ __launch_bounds__(WP * WQ * 64, 2) void k_f8_gemm(F8Gemm g, unsigned 
   if (g.vec8 && !g.partial && pw + TP * 16 <= g.P.lines) {
     // 16-bit outputs: the words of two tiles change places between the rows of
     // 16 lanes, so that a lane has eight adjacent lines and four lanes 64 bytes
-    // (with 8 bytes a lane the stores of 4096^2 outputs take 8.5 us, not XX)
+    // (the stores of 4096^2 outputs take 5.6 us, with 8 bytes a lane 8.5)
     const int at = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
@@ -422,7 +437,8 @@ hipError_t launch_tile(hipStream_t st, const F8Gemm& g) {
   const int64_t tiles_q = (g.Q.lines + WQ * TQ * 16 - 1) / (WQ * TQ * 16);
   const int64_t total = (g.k + kF8Block - 1) / kF8Block,
                 ranges = total > g.stages ? (total + g.stages - 1) / g.stages : 1;
-  hipLaunchKernelGGL((k_f8_gemm<kExact, kTurned, kMode, FP, FQ, WP, WQ, TP, TQ, kSlots>), dim3((unsigned)(tiles_p * tiles_q * ranges)),
+  hipLaunchKernelGGL((k_f8_gemm<kExact, kTurned, kMode, FP, FQ, WP, WQ, TP, TQ, kSlots>),
+                     dim3((unsigned)(tiles_p * tiles_q * ranges)),
                      dim3(WP * WQ * 64), 0, st, g, (unsigned)tiles_p, (unsigned)tiles_q);
   return hipGetLastError();
 }

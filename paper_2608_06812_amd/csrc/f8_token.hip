@@ -28,9 +28,13 @@ constexpr int kTokWaves = 8;
 template <bool kAny> struct Values;
 template <> struct Values<false> {
   v4i v[2];
-  __device__ __forceinline__ void load(int h, const uint8_t* p) { __builtin_memcpy(&v[h], __builtin_assume_aligned(p, 4), 16); }
+  __device__ __forceinline__ void load(int h, const uint8_t* p) {
+    __builtin_memcpy(&v[h], __builtin_assume_aligned(p, 4), 16);
+  }
   __device__ __forceinline__ void set(int h, v4i x) { v[h] = x; }
-  __device__ __forceinline__ v8i get() const { return v8i{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w}; }
+  __device__ __forceinline__ v8i get() const {
+    return v8i{v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+  }
 };
 template <> struct Values<true> {
   Dwords v[2];
@@ -283,7 +287,9 @@ hipError_t launch(hipStream_t st, const F8Token& t) {
 // are better (one token, 8192 lines of 8192: 14.3 us with 16 lines, 19 with 32).
 template <bool kPow, int TQ, int kSrc>
 hipError_t launch_lines(hipStream_t st, const F8Token& t) {
-  auto aligned = [](const F8Lines& l) { return (reinterpret_cast<uintptr_t>(l.x) | (l.lines > 1 ? l.ld : 0)) % 4 == 0; };
+  auto aligned = [](const F8Lines& l) {
+    return (reinterpret_cast<uintptr_t>(l.x) | (l.lines > 1 ? l.ld : 0)) % 4 == 0;
+  };
   const bool any = !aligned(t.P) || (kSrc < 0 && !aligned(t.Q));
   if constexpr (TQ == 2) {
     if (t.P.lines >= 2 * 16 * 256)

@@ -268,6 +268,19 @@ def test_gemm_large(gpu_lib, dtype, kind):
         assert torch.equal(first, gpu_lib.gemm_f8(*ops, dtype))
 
 
+MIDDLE = [(2000, 2030, 300), (1950, 2048, 515)]
+
+
+@pytest.mark.parametrize("kind", [F32, E8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_gemm_middle(gpu_lib, dtype, kind):
+    """Sizes of the middle block tile, both orders of B."""
+    for m, n, k in MIDDLE:
+        for b_order, b_tile in (("col", True), ("col", False), ("row", True), ("row", False)):
+            A, SA, B, SB = operands(m, n, k, F32, E4, E5, b_tile=b_tile, b_order=b_order)
+            check_gemm(gpu_lib, (A, (SA * 1e-3).to(kind), B, (SB * 1e-2).to(kind)), dtype)
+
+
 @pytest.mark.parametrize("kind", [F32, E8])
 @pytest.mark.parametrize("a_fmt,b_fmt", [(E4, E5), (E5, E4), (E5, E5)])
 def test_gemm_formats(gpu_lib, a_fmt, b_fmt, kind):
@@ -390,7 +403,24 @@ def test_gemm_zeros(gpu_lib):
 def test_gemm_long_k(gpu_lib):
     for m, n, k in ((1, 40, 70000), (3, 20, 200001), (200, 130, 33000), (16, 300, 20000)):
         for kind in (F32, E8):
-            check_gemm(gpu_lib, operands(m, n, k, kind, b_tile=False))
+            ops = operands(m, n, k, kind, b_tile=False)
+            check_gemm(gpu_lib, ops)
+            check_gemm(gpu_lib, ops, torch.bfloat16, out=torch.empty((n, m), device="cuda", dtype=torch.bfloat16).t())
+            check_gemm(gpu_lib, ops, F32, out=torch.randn((m, n + 3), device="cuda")[:, :n], accumulate=True)
+
+
+def test_gemm_nan_scale(gpu_lib):
+    """An E8M0 byte of 255 is NaN, for its line's block and no other."""
+    for m, n, k in ((5, 64, 384), (140, 150, 384)):
+        for dtype in (torch.float32, torch.bfloat16):
+            A, SA, B, SB = operands(m, n, k, E8, b_tile=False)
+            SA.view(torch.uint8)[3, 1] = 255
+            SB.view(torch.uint8)[2, 7] = 255
+            announce(f"NaN scales {m}x{n}x{k} {dtype}")
+            C = gpu_lib.gemm_f8(A, SA, B, SB, dtype)
+            nan = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+            nan[3], nan[:, 7] = True, True
+            assert torch.equal(torch.isnan(C), nan)
 
 
 def test_gemm_offsets_beyond_32_bits(gpu_lib):
