@@ -102,15 +102,15 @@ __device__ __forceinline__ v8i read_turned(const uint8_t* from) {
 // scales of a stage, one word a line (a byte is extended on its way), are copied
 // likewise.
 //
-// 256 x 256 tiles with two slots, for outputs of 16 bits, need 16 bytes of
-// operands a cycle and CU; 256 x 128 with three, where the BF16 form takes twice
-// the matrix cycles, as many. At 8192^3 they keep the matrix cores 68 % busy (BF16
-// 69 %) at 1.74 GHz (2.1), where the power limit holds the chip: 2.50 PFLOP/s with
-// FP32 scales, 2.77 with powers of two, and 1.16 and 1.25 to FP32, beside 2.82 and
-// 1.31 of the library's products with one scale for all. A weight gradient with a
-// scale a line on both sides (4096 x 4096 x 16384: 1.05 PFLOP/s) is bound by the
-// vector instructions that scale and convert: 70 % of the issue cycles beside 49 %
-// of the matrix cores'.
+// 256 x 256 tiles with two slots, for outputs of 16 bits, copy 64 KiB for 2048
+// matrix cycles a SIMD; 256 x 128 with three, where the BF16 form takes twice the
+// cycles, 48 KiB. At 8192^3 the first keep the matrix cores 68 % busy (74 % with
+// powers of two) at 1.74 GHz, where the power limit holds the chip: 2.44-2.50
+// PFLOP/s with FP32 scales, 2.67-2.77 with powers of two, and 1.14 and 1.24 to
+// FP32, beside 2.82 and 1.31 of the library's products with one scale for all. A
+// weight gradient with a scale a line on both sides (4096 x 4096 x 16384: 1.05
+// PFLOP/s) is bound by the vector instructions that scale and convert: 71 % of the
+// issue cycles beside 49 % of the matrix cores'.
 //
 // kTurned: P's lines are adjacent where its k values would be (the weights of a
 // layer in the product with an output gradient): rows of k, P.ld bytes apart. A
@@ -445,11 +445,14 @@ hipError_t launch_tile(hipStream_t st, const F8Gemm& g) {
 
 template <bool kExact, bool kTurned, int kMode, int FP, int FQ>
 hipError_t launch_size(hipStream_t st, const F8Gemm& g) {
+  // two blocks a CU of the smaller tiles: the middle one with two slots (with four
+  // and one block 2048^3 takes 17.2 us in place of 15.2); the small one's four
+  // cover the latency of its short stages
   switch (g.tile) {
     case kF8Tile256:
       if constexpr (kExact) return launch_tile<kExact, kTurned, kMode, FP, FQ, 4, 2, 4, 4, 3>(st, g);
       else return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 4, 8, 4, 2>(st, g);
-    case kF8Tile128: return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 2, 4, 4, 4>(st, g);
+    case kF8Tile128: return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 2, 4, 4, 2>(st, g);
     default: return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 2, 2, 2, 4>(st, g);
   }
 }

@@ -165,7 +165,7 @@ inline F8TileTimes f8_times(F8Tile tile, bool exact) {
     case kF8Tile64:
       return exact ? F8TileTimes{64, 64, 512, 0.49, 0.77, 2.5} : F8TileTimes{64, 64, 512, 0.30, 0.50, 2.5};
     case kF8Tile128:
-      return exact ? F8TileTimes{128, 128, 256, 1.02, 1.40, 3.0} : F8TileTimes{128, 128, 256, 0.66, 0.94, 3.0};
+      return exact ? F8TileTimes{128, 128, 256, 1.02, 1.38, 3.0} : F8TileTimes{128, 128, 256, 0.66, 0.80, 3.0};
     default: return exact ? F8TileTimes{256, 128, 256, 1.50, 1.75, 6.0} : F8TileTimes{256, 256, 256, 1.28, 1.60, 5.5};
   }
 }
