@@ -24,47 +24,39 @@ __global__ __launch_bounds__(256) void k_f8_pack(F8PackPair two) {
   const F8Pack p = which ? two.p[1] : two.p[0];
   const unsigned b = blockIdx.x - (which ? two.first : 0), nl = two.tiles[which];
   const int64_t l0 = (int64_t)(b % nl) * kPackTile, k0 = (int64_t)(b / nl) * kPackTile;
-  const int t = threadIdx.x, sub = t & 31, row = t >> 5;   // 4 bytes of a row of the tile, 8 rows a pass
-  if (p.ks == 1) {
-    // all loads before the first use, those of a line's end too: the 16 bytes
-    // that end with it
-    Dwords d[4];
+  const int t = threadIdx.x, sub = t & 31, row = t >> 5;
+  // rows along the unit stride: of k values, or of lines
+  const bool along_k = p.ks == 1;
+  const int64_t a0 = along_k ? l0 : k0, as = along_k ? p.ls : p.ks, an = along_k ? p.lines : p.k;
+  const int64_t u0 = (along_k ? k0 : l0) + (t & 7) * 16, un = along_k ? p.k : p.lines;
+  // all loads before the first use, those of a row's end too: the 16 bytes that
+  // end with it
+  Dwords d[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
-      if (line < p.lines && kk < p.k && p.k >= 16) d[n] = load_dwords(p.x + line * p.ls + min(kk, p.k - 16));
-    }
+  for (int n = 0; n < 4; ++n) {
+    const int64_t a = a0 + n * 32 + (t >> 3);
+    if (a < an && u0 < un && un >= 16) d[n] = load_dwords(p.x + a * as + min(u0, un - 16));
+  }
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int64_t line = l0 + n * 32 + (t >> 3), kk = k0 + (t & 7) * 16;
-      if (line >= p.lines || kk >= p.k) continue;
-      v4i v;
-      if (p.k >= 16) {
+  for (int n = 0; n < 4; ++n) {
+    const int r = n * 32 + (t >> 3);
+    const int64_t a = a0 + r;
+    v4i v = {0, 0, 0, 0};
+    if (a < an && u0 < un) {
+      if (un >= 16) {
         v = d[n].bytes();
-        if (kk + 16 > p.k) v = last_bytes(v, (int)(p.k - kk));
+        if (u0 + 16 > un) v = last_bytes(v, (int)(un - u0));
       } else {
-        const uint8_t* from = p.x + line * p.ls;
-        v = load_end(from, from + kk, (int)(p.k - kk));
+        const uint8_t* from = p.x + a * as;
+        v = load_end(from, from + u0, (int)(un - u0));
       }
-      *reinterpret_cast<v4i*>(p.out + line * p.ld + kk) = v;
+      if (along_k) *reinterpret_cast<v4i*>(p.out + a * p.ld + u0) = v;
     }
-    return;
-  }
+    if (!along_k)
 #pragma unroll
-  for (int n = 0; n < 16; ++n) {
-    const int r = n * 8 + row;
-    const int64_t a = k0 + r, u = l0 + sub * 4;
-    uint32_t w = 0;
-    if (a < p.k) {
-      const uint8_t* src = p.x + a * p.ks + u;
-      if (u + 4 <= p.lines)
-        __builtin_memcpy(&w, src, 4);
-      else
-        for (int e = 0; e < 4; ++e)
-          if (u + e < p.lines) w |= (uint32_t)src[e] << (8 * e);
-    }
-    *reinterpret_cast<uint32_t*>(tile + r * kPackLd + sub * 4) = w;
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<int*>(tile + r * kPackLd + (t & 7) * 16 + e * 4) = v[e];
   }
+  if (along_k) return;
   __syncthreads();
   // four k values of a line a thread
 #pragma unroll
