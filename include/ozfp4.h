@@ -256,9 +256,9 @@ typedef struct {
  * the rows axis: values with rs = 1, cs >= rows. So values are adjacent along
  * the axis that a product will sum over; that stride is a multiple of 16 and
  * the values are 16-byte aligned (else OZFP4_EINVAL), and bytes up to the
- * multiple of 16 behind a line's end are overwritten. Both outputs have one format
- * and one `tile`; both are made from one read of X. Asynchronous on the set
- * stream, allocates nothing, and so can be captured into a graph.
+ * multiple of 16 behind a line's end are overwritten. Both outputs have one
+ * format and one `tile`; both are made from one read of X. Asynchronous on the
+ * set stream, allocates nothing, and so can be captured into a graph.
  */
 int ozfp4_quantize_f8(int64_t rows, int64_t cols, const void* X, int x_type, int64_t x_rs, int64_t x_cs,
                       int scale_type, const ozfp4_f8_matrix* along_cols, const ozfp4_f8_matrix* along_rows);
@@ -272,8 +272,9 @@ int ozfp4_quantize_f8(int64_t rows, int64_t cols, const void* X, int x_type, int
  * and B). An FP32 C is as exact as FP32 additions make it. For 16-bit C the
  * matrix cores may add eight neighbouring products at a time with 13 bits below
  * the largest: off by 2e-5 to 5e-5 of typical results (the rounding of C is
- * 2e-4 and more), at most 2^-10 of the sum of the terms' magnitudes. accumulate: C (FP32) += A B. NaN and infinities propagate as in
- * FP32 arithmetic. k = 0 writes zeros (adds nothing).
+ * 2e-4 and more), at most 2^-10 of the sum of the terms' magnitudes.
+ * accumulate: C (FP32) += A B. NaN and infinities propagate as in FP32
+ * arithmetic. k = 0 writes zeros (adds nothing).
  * Operands whose k values are adjacent, with lines 16-byte aligned and at
  * most 2^23 bytes apart, are read in place, and so is, in either order, the one
  * along whose lines C is adjacent (B for a row-major C); others are copied into

@@ -1,6 +1,6 @@
 // 8-bit floating-point products with a scale for each block of 128: host
-// interface of the kernels in f8_quantize.hip, f8_pack.hip and f8_gemm.hip,
-// and the device helpers that they share.
+// interface of the kernels in f8_quantize.hip, f8_pack.hip, f8_gemm.hip and
+// f8_token.hip.
 //
 // A quantised matrix holds e4m3 or e5m2 values and one scale for every block
 // of 128 along the contraction: per line (1 x 128) or per 128 x 128 tile.

@@ -22,9 +22,6 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < __builtin_inff() ? a : 0.0f;
 }
 
-// max(m, |x|); drops NaN but not infinities
-__device__ __forceinline__ float max_abs(float m, float x) { return __builtin_fmaxf(m, __builtin_fabsf(x)); }
-
 // A block's scale and what its elements need: S = m 2^e, m in [1, 2), and r,
 // 1 / m to an ulp.
 struct Scale {
