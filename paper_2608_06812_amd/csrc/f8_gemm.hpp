@@ -103,14 +103,16 @@ __device__ __forceinline__ v8i read_turned(const uint8_t* from) {
 // likewise.
 //
 // 256 x 256 tiles with two slots, for outputs of 16 bits, copy 64 KiB for 2048
-// matrix cycles a SIMD; 256 x 128 with three, where the BF16 form takes twice the
-// cycles, 48 KiB. At 8192^3 the first keep the matrix cores 68 % busy (74 % with
-// powers of two) at 1.74 GHz, where the power limit holds the chip: 2.44-2.50
-// PFLOP/s with FP32 scales, 2.67-2.77 with powers of two, and 1.14 and 1.24 to
-// FP32, beside 2.82 and 1.31 of the library's products with one scale for all. A
-// weight gradient with a scale a line on both sides (4096 x 4096 x 16384: 1.05
-// PFLOP/s) is bound by the vector instructions that scale and convert: 71 % of the
-// issue cycles beside 49 % of the matrix cores'.
+// matrix cycles a SIMD; the BF16 form takes twice the cycles, and two blocks a CU
+// of 128 x 128 tiles cover each other's conversions, barriers and output (256 x
+// 128 tiles with three slots, one block a CU: 8192^3 919 us in place of 890,
+// 3000^3 89 in place of 67). At 8192^3 the first keep the matrix cores 68 % busy
+// (74 % with powers of two) at 1.74 GHz, where the power limit holds the chip:
+// 2.44-2.50 PFLOP/s with FP32 scales, 2.67-2.77 with powers of two, and 1.24 and
+// 1.31 to FP32, beside 2.82 and 1.31 of the library's products with one scale for
+// all. A weight gradient with a scale a line on both sides (4096 x 4096 x 16384:
+// 1.05-1.15 PFLOP/s) is bound by the vector instructions that scale and convert:
+// 71 % of the issue cycles beside 49 % of the matrix cores'.
 //
 // kTurned: P's lines are adjacent where its k values would be (the weights of a
 // layer in the product with an output gradient): rows of k, P.ld bytes apart. A
@@ -449,8 +451,8 @@ hipError_t launch_size(hipStream_t st, const F8Gemm& g) {
   // and one block 2048^3 takes 17.2 us in place of 15.2); the small one's four
   // cover the latency of its short stages
   switch (g.tile) {
-    case kF8Tile256:
-      if constexpr (kExact) return launch_tile<kExact, kTurned, kMode, FP, FQ, 4, 2, 4, 4, 3>(st, g);
+    case kF8Tile256:   // not of the exact form (f8_route)
+      if constexpr (kExact) return hipErrorInvalidValue;
       else return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 4, 8, 4, 2>(st, g);
     case kF8Tile128: return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 2, 4, 4, 2>(st, g);
     default: return launch_tile<kExact, kTurned, kMode, FP, FQ, 2, 2, 2, 2, 4>(st, g);

@@ -143,9 +143,9 @@ inline bool use_short_ozi(int64_t m, int64_t n, int64_t k, int nh) {
 }
 
 // ------------------------------------------------------------ 8-bit products
-// Block tile and k ranges of an 8-bit product (f8_gemm.hip): 64 x 64 (two
-// blocks a CU), 128 x 128, or 256 x 256 (256 x 128 in the exact form, which
-// FP32 outputs take).
+// Block tile and k ranges of an 8-bit product (f8_gemm.hip): 64 x 64 and 128 x
+// 128, two blocks a CU, or 256 x 256, one; the exact form, which FP32 outputs
+// take, has the first two.
 enum F8Tile { kF8Tile64, kF8Tile128, kF8Tile256 };
 struct F8Route {
   F8Tile tile;
@@ -153,36 +153,38 @@ struct F8Route {
 };
 constexpr int kF8MaxRanges = 16;
 
-// Measured in us: a stage (128 of k) of a block with the chip almost empty and
-// with `blocks` running, and what a block takes around its stages (its first
-// copies; its output, which all blocks write at about the same time).
+// Measured in us: a stage (128 of k) of a block with the chip almost empty, with
+// a block on each of the 256 CUs and with `blocks` running, and what a block takes
+// around its stages (its first copies; its output, which all blocks write at
+// about the same time).
 struct F8TileTimes {
-  int p, q, blocks;
-  double alone, full, around;
+  int side, blocks;
+  double alone, one, full, around;
 };
 inline F8TileTimes f8_times(F8Tile tile, bool exact) {
   switch (tile) {
-    case kF8Tile64:
-      return exact ? F8TileTimes{64, 64, 512, 0.49, 0.77, 2.5} : F8TileTimes{64, 64, 512, 0.30, 0.50, 2.5};
+    case kF8Tile64: return exact ? F8TileTimes{64, 512, 0.48, 0.51, 0.72, 2.5} : F8TileTimes{64, 512, 0.29, 0.31, 0.47, 2.5};
     case kF8Tile128:
-      return exact ? F8TileTimes{128, 128, 256, 1.02, 1.38, 3.0} : F8TileTimes{128, 128, 256, 0.66, 0.80, 3.0};
-    default: return exact ? F8TileTimes{256, 128, 256, 1.50, 1.75, 6.0} : F8TileTimes{256, 256, 256, 1.28, 1.60, 5.5};
+      return exact ? F8TileTimes{128, 512, 0.94, 1.15, 1.75, 5.0} : F8TileTimes{128, 512, 0.47, 0.68, 1.0, 4.3};
+    default: return F8TileTimes{256, 256, 1.2, 1.6, 1.6, 7.0};
   }
 }
 
 // Estimated time: whole rounds of blocks, and the blocks that are left; with
 // ranges a second kernel and the partial sums' traffic. Against measured times
-// (16-bit output; 64, 128, 256 tiles): 3000^3 69, 71, 41 / 65, 64, 42; 2500^3
-// 46, 41, 34 / 42, 38, 38; 1024 x 8192 x 2048 42, 36, 29 / 35, 33, 32; 1024 x 1024 x
-// 4096 in one range and two of 64 tiles 13.6, 17.9 / 13.0, 17.8; 512 x 512 x 8192
-// in one, four, eight ranges 22, 13.1, 13.9 / 21, 12.7, 15.1.
+// (16-bit output; 64, 128, 256 tiles): 3000^3 65, 45, 41 / 61, 49, 41; 2500^3 44,
+// 24, 34 / 43, 29, 37; 2048 x 4096 x 4096 70, 36, 52 / 57, 37, 47; 4096 x 8192 x
+// 1024 100, 49, 40 / 71, 45, 39; 1024 x 1024 x 4096 in one range and two of 64
+// tiles 12.4, 17.4 / 12.5, 17.3; 512 x 512 x 8192 in one, two, four ranges 21,
+// 16.9, 13.1 / 20, 15.7, 13.0. Over 46 products the choices take 0.4 % more than
+// the best of these tiles.
 inline double f8_us(int64_t lines_p, int64_t lines_q, int64_t k, F8Tile tile, int ranges, bool exact) {
   const F8TileTimes t = f8_times(tile, exact);
   const int64_t all = tiles(k, 128), stages = (all + ranges - 1) / ranges;
-  const int64_t blocks = tiles(lines_p, t.p) * tiles(lines_q, t.q) * ranges;
+  const int64_t blocks = tiles(lines_p, t.side) * tiles(lines_q, t.side) * ranges;
   const int64_t rounds = blocks / t.blocks, rest = blocks % t.blocks;
   double us = (double)rounds * ((double)stages * t.full + t.around);
-  if (rest > 0) us += (double)stages * (t.alone + (t.full - t.alone) * (double)rest / t.blocks) + t.around;
+  if (rest > 0) us += (double)stages * (rest > 256 ? t.full : t.alone + (t.one - t.alone) * (double)rest / 256) + t.around;
   if (ranges > 1) us += 4.0 + (double)ranges * (double)lines_p * (double)lines_q * 8.0 / 5e6;
   return us;
 }
@@ -190,7 +192,8 @@ inline double f8_us(int64_t lines_p, int64_t lines_q, int64_t k, F8Tile tile, in
 inline F8Route f8_route(int64_t lines_p, int64_t lines_q, int64_t k, bool exact) {
   F8Route best = {kF8Tile64, 1};
   double least = -1;
-  for (F8Tile tile : {kF8Tile256, kF8Tile128, kF8Tile64})
+  for (F8Tile tile : {kF8Tile256, kF8Tile128, kF8Tile64}) {
+    if (exact && tile == kF8Tile256) continue;
     for (int ranges = 1; ranges <= kF8MaxRanges && (ranges == 1 || tiles(k, 128) / ranges >= 4); ++ranges) {
       const double us = f8_us(lines_p, lines_q, k, tile, ranges, exact);
       if (least < 0 || us < least) {
@@ -198,6 +201,7 @@ inline F8Route f8_route(int64_t lines_p, int64_t lines_q, int64_t k, bool exact)
         best = {tile, ranges};
       }
     }
+  }
   return best;
 }
 
