@@ -106,13 +106,14 @@ __device__ __forceinline__ v8i read_turned(const uint8_t* from) {
 // matrix cycles a SIMD; the BF16 form takes twice the cycles, and two blocks a CU
 // of 128 x 128 tiles cover each other's conversions, barriers and output (256 x
 // 128 tiles with three slots, one block a CU: 8192^3 919 us in place of 890,
-// 3000^3 89 in place of 67). At 8192^3 the first keep the matrix cores 68 % busy
-// (74 % with powers of two) at 1.74 GHz, where the power limit holds the chip:
-// 2.44-2.50 PFLOP/s with FP32 scales, 2.67-2.77 with powers of two, and 1.24 and
-// 1.31 to FP32, beside 2.82 and 1.31 of the library's products with one scale for
-// all. A weight gradient with a scale a line on both sides (4096 x 4096 x 16384:
-// 1.05-1.15 PFLOP/s) is bound by the vector instructions that scale and convert:
-// 71 % of the issue cycles beside 49 % of the matrix cores'.
+// 3000^3 89 in place of 67; with a scale a line on both sides 4096 x 4096 x 16384
+// 519 against 528). At 8192^3 the first keep the matrix cores 68 % busy (73 % with
+// powers of two) at 1.74 GHz, where the power limit holds the chip: 2.4-2.5
+// PFLOP/s with FP32 scales, 2.67-2.77 with powers of two, and 1.18-1.24 and
+// 1.27-1.31 to FP32, beside 2.82 and 1.31 of the library's products with one scale
+// for all. The weight gradient with a scale a line on both sides (1.01-1.14
+// PFLOP/s) is bound by the vector instructions that scale and convert: 71 % of the
+// issue cycles beside 51 % of the matrix cores'.
 //
 // kTurned: P's lines are adjacent where its k values would be (the weights of a
 // layer in the product with an output gradient): rows of k, P.ld bytes apart. A

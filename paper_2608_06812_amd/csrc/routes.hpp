@@ -163,7 +163,8 @@ struct F8TileTimes {
 };
 inline F8TileTimes f8_times(F8Tile tile, bool exact) {
   switch (tile) {
-    case kF8Tile64: return exact ? F8TileTimes{64, 512, 0.48, 0.51, 0.72, 2.5} : F8TileTimes{64, 512, 0.29, 0.31, 0.47, 2.5};
+    case kF8Tile64:
+      return exact ? F8TileTimes{64, 512, 0.48, 0.51, 0.72, 2.5} : F8TileTimes{64, 512, 0.29, 0.31, 0.47, 2.5};
     case kF8Tile128:
       return exact ? F8TileTimes{128, 512, 0.94, 1.15, 1.75, 5.0} : F8TileTimes{128, 512, 0.47, 0.68, 1.0, 4.3};
     default: return F8TileTimes{256, 256, 1.2, 1.6, 1.6, 7.0};
@@ -184,7 +185,8 @@ inline double f8_us(int64_t lines_p, int64_t lines_q, int64_t k, F8Tile tile, in
   const int64_t blocks = tiles(lines_p, t.side) * tiles(lines_q, t.side) * ranges;
   const int64_t rounds = blocks / t.blocks, rest = blocks % t.blocks;
   double us = (double)rounds * ((double)stages * t.full + t.around);
-  if (rest > 0) us += (double)stages * (rest > 256 ? t.full : t.alone + (t.one - t.alone) * (double)rest / 256) + t.around;
+  if (rest > 0)
+    us += (double)stages * (rest > 256 ? t.full : t.alone + (t.one - t.alone) * (double)rest / 256) + t.around;
   if (ranges > 1) us += 4.0 + (double)ranges * (double)lines_p * (double)lines_q * 8.0 / 5e6;
   return us;
 }

@@ -56,3 +56,6 @@ def test_gpu_cases_reach_every_tile(route):
     # the 128 x 128 tile: sizes of test_gemm_middle
     for exact in (False, True):
         assert [t for t, _ in route([(n, m, k, exact) for m, n, k in gpu.MIDDLE])] == [1] * len(gpu.MIDDLE)
+    # k ranges of the larger tiles: sizes of test_gemm_ranges
+    got = route([(n, m, k, dtype.itemsize == 4) for m, n, k, dtype in gpu.RANGES])
+    assert [(t, r > 1) for t, r in got] == [(1, True), (1, True), (2, True)]

@@ -281,6 +281,18 @@ def test_gemm_middle(gpu_lib, dtype, kind):
             check_gemm(gpu_lib, (A, (SA * 1e-3).to(kind), B, (SB * 1e-2).to(kind)), dtype)
 
 
+# 128 x 128 tiles with k ranges, of FP32 and of 16-bit outputs, and 256 x 256 tiles
+RANGES = [(677, 965, 5669, torch.float32), (674, 1520, 5828, torch.bfloat16), (1460, 1801, 12623, torch.bfloat16)]
+
+
+@pytest.mark.parametrize("kind", [F32, E8])
+@pytest.mark.parametrize("m,n,k,dtype", RANGES)
+def test_gemm_ranges(gpu_lib, m, n, k, dtype, kind):
+    """k ranges of the larger block tiles, both orders of B."""
+    for b_order, b_tile in (("col", True), ("row", False)):
+        check_gemm(gpu_lib, operands(m, n, k, kind, E4, E4, b_tile=b_tile, b_order=b_order), dtype)
+
+
 @pytest.mark.parametrize("kind", [F32, E8])
 @pytest.mark.parametrize("a_fmt,b_fmt", [(E4, E5), (E5, E4), (E5, E5)])
 def test_gemm_formats(gpu_lib, a_fmt, b_fmt, kind):
